@@ -522,6 +522,70 @@ usv_status usv_block_sparse_attn_fused(const void* q, const void* k, const void*
                                        const void* gate_fine, const void* gate_coarse,
                                        int32_t out_dtype, void* out, float* lse, void* stream);
 
+/*
+ * Attention over a window with sinks, on tensors in the order of their positions (raster order: frame after frame).  It
+ * is the fixed sparsity pattern of a causal or streaming student: a frame sees the frames around it and the first ones.
+ * Tokens are grouped in chunks of `chunk` consecutive positions (the tokens of a frame; 1 = single tokens).  In a
+ * sequence of n tokens the query at position p sees the key at position j, both in [0, n), iff
+ *   chunk(j) <= chunk(p) + right   and   (chunk(j) >= chunk(p) - left  or  chunk(j) < sinks)
+ * with chunk(x) = x / chunk; a negative left or right is no limit on that side.
+ *   out[b,h,i,:] = sum_j softmax_j(scale q_i . k_j) v_j        over the keys that query i sees
+ * Query row i of batch element b is at position q_start + i, or, with q_start = USV_Q_AT_END, at n - q_len + i (the
+ * queries are the newest tokens).  n = seq_lens[b], or kv_len without seq_lens.  Query rows at positions outside [0, n)
+ * hold no token: out is 0 there and lse -inf; every other row sees its own position at least.  Key rows that no query of
+ * a call sees and query rows without a token may hold anything, infinities and NaN among it; the others must be finite.
+ * Query heads h share the key head h / (q_heads / kv_heads).
+ */
+#define USV_Q_AT_END INT32_MIN
+typedef struct {
+  int32_t batch;            /* B >= 1 */
+  int32_t q_heads, kv_heads; /* kv_heads >= 1 divides q_heads */
+  int32_t q_len, kv_len;    /* rows of q and of k, v per head: 0 .. 2^30 */
+  int32_t head_dim;         /* 64 or 128 */
+  int32_t dtype;            /* usv_dtype of every tensor but lse */
+  int32_t left, right;      /* chunks before and after a query's own that it sees, at most 2^30; negative: all */
+  int32_t sinks;            /* first chunks that stay visible, 0 .. 2^30 */
+  int32_t chunk;            /* positions of a chunk, 1 .. 2^30 */
+  int32_t q_start;          /* position of query row 0, at most 2^30 away from 0, or USV_Q_AT_END */
+  const int32_t* seq_lens;  /* NULL, or device [B]: tokens of each sequence, clamped into [0, kv_len] */
+  usv_strides q, k, v, out; /* element strides; token == 0 means contiguous [B, heads, len, d].  A stride times the element
+                               size is a multiple of 16 bytes; rows of out must not overlap */
+} usv_window;
+
+/* Bytes of device scratch usv_window_attn uses for `w`: 0 where the rows fill the chip; otherwise the keys are shared
+ * out and the pieces joined.  (0 also for an invalid `w`.) */
+size_t usv_window_workspace_bytes(const usv_window* w);
+
+/* q [B, q_heads, q_len, d], k, v [B, kv_heads, kv_len, d] (device, read only), out like q (written), all of w->dtype.
+ * scale : softmax scale; <= 0 selects 1/sqrt(d)
+ * lse   : NULL or [B, q_heads, q_len] fp32 (written): natural-log sum of exp of the scaled logits
+ * ws    : NULL, or device scratch of at least usv_window_workspace_bytes(w) (contents on return unspecified); without it
+ *         a call of few rows takes longer.
+ * bf16: products on bf16 MFMA with fp32 accumulation, the weights rounded to bf16 before they meet V, their sum taken
+ * unrounded in fp32.  fp32: fp32 products and sums.  The same call gives the same bits every time. */
+usv_status usv_window_attn(const void* q, const void* k, const void* v, const usv_window* w, float scale, void* out,
+                           float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Strides of the gradients (as those of usv_window; token == 0 means contiguous). */
+typedef struct {
+  usv_strides dout, dq, dk, dv;
+} usv_window_grads;
+
+/* Bytes of device scratch usv_window_attn_backward needs for `w`; 0 for an invalid `w`. */
+size_t usv_window_backward_workspace_bytes(const usv_window* w);
+
+/* Gradients of usv_window_attn: with P = exp(scale q.k - lse), D = sum over the channels of dout * out,
+ *   dS = P (dout.v - D),  dq = scale dS k,  dk = scale dS^T q,  dv = P^T dout,
+ * dk and dv summed over the query heads that share a key head.
+ * q, k, v, out, lse : as given to and written by usv_window_attn with the same `w` and scale (device, read only)
+ * dout  : [B, q_heads, q_len, d] of w->dtype (device, read only); rows without a token may hold anything
+ * dq, dk, dv : the shapes of q, k, v, of w->dtype (written); rows that see nothing or are seen by no query are 0
+ * ws    : device scratch >= usv_window_backward_workspace_bytes(w); contents on return unspecified
+ * No atomics: the same call gives the same bits every time. */
+usv_status usv_window_attn_backward(const void* q, const void* k, const void* v, const void* out, const float* lse,
+                                    const void* dout, const usv_window* w, const usv_window_grads* grads, float scale,
+                                    void* dq, void* dk, void* dv, void* ws, size_t ws_bytes, void* stream);
+
 /* Static string for a status code. */
 const char* usv_status_string(int32_t status);
 

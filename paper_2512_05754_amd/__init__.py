@@ -27,6 +27,9 @@ _BINDING_NAMES = (
     "cube_token_order",
     "cube_gather",
     "cube_scatter",
+    "window_attn",
+    "window_attn_backward",
+    "window_workspace_bytes",
     "workspace_bytes",
     "lib",
     "lib_path",

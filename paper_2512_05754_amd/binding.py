@@ -6,6 +6,7 @@ There is no CPU fallback: a missing library or a CPU tensor raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import hashlib
 import importlib.machinery
@@ -53,6 +54,10 @@ EXPORTED_SYMBOLS = (
     "usv_cube_token_order",
     "usv_cube_gather",
     "usv_cube_scatter",
+    "usv_window_workspace_bytes",
+    "usv_window_attn",
+    "usv_window_backward_workspace_bytes",
+    "usv_window_attn_backward",
     "usv_status_string",
     "usv_last_error",
 )
@@ -88,6 +93,18 @@ class UsvStrides(ctypes.Structure):
 class UsvRaster(ctypes.Structure):
     _fields_ = [("order", ctypes.c_void_p), ("in_strides", UsvStrides), ("out_strides", UsvStrides),
                 ("block_valid", ctypes.c_void_p), ("work_order", ctypes.c_void_p)]
+
+
+USV_Q_AT_END = -(1 << 31)
+
+
+class UsvWindow(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "q_heads", "kv_heads", "q_len", "kv_len", "head_dim", "dtype", "left", "right", "sinks", "chunk", "q_start")]
+    _fields_ += [("seq_lens", ctypes.c_void_p)] + [(n, UsvStrides) for n in ("q", "k", "v", "out")]
+
+
+class UsvWindowGrads(ctypes.Structure):
+    _fields_ = [(n, UsvStrides) for n in ("dout", "dq", "dk", "dv")]
 
 
 def lib_path() -> str:
@@ -189,6 +206,12 @@ def lib() -> ctypes.CDLL:
     L.usv_coarse_attn_raster.restype, L.usv_coarse_attn_raster.argtypes = i32, [vp, vp, sp, rp, vp, vp, sz, vp]
     L.usv_block_sparse_attn_raster_fused.restype = i32
     L.usv_block_sparse_attn_raster_fused.argtypes = [vp, vp, vp, sp, rp, vp, vp, i32, f32, vp, vp, vp, i32, vp, vp, vp]
+    wp = ctypes.POINTER(UsvWindow)
+    L.usv_window_workspace_bytes.restype, L.usv_window_workspace_bytes.argtypes = sz, [wp]
+    L.usv_window_attn.restype, L.usv_window_attn.argtypes = i32, [vp, vp, vp, wp, f32, vp, vp, vp, sz, vp]
+    L.usv_window_backward_workspace_bytes.restype, L.usv_window_backward_workspace_bytes.argtypes = sz, [wp]
+    L.usv_window_attn_backward.restype = i32
+    L.usv_window_attn_backward.argtypes = [vp, vp, vp, vp, vp, vp, wp, ctypes.POINTER(UsvWindowGrads), f32, vp, vp, vp, vp, sz, vp]
     L.usv_status_string.restype, L.usv_status_string.argtypes = ctypes.c_char_p, [i32]
     L.usv_last_error.restype, L.usv_last_error.argtypes = ctypes.c_char_p, []
     if calls is not None:
@@ -743,6 +766,136 @@ def block_sparse_attn_raster(q, k, v, order, idx, cnt, scale=0.0, out=None, out_
         int(idx.shape[3]), float(scale), None if coarse is None else _dev(coarse, "coarse", torch.float32), gates[0],
         gates[1], _dt(out), op, None if lse is None else _dev(lse, "lse", torch.float32), _stream()))
     return (out, lse) if return_lse else out
+
+
+def _rows(t: torch.Tensor, name: str, like: torch.Tensor, shape=None):
+    """Pointer and element strides of a [B, heads, len, d] tensor with contiguous channels, of `like`'s type and device."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor (there is no CPU path)")
+    if t.dim() != 4 or (t.stride(3) != 1 and t.numel() > 0):
+        raise ValueError(f"{name} must be [B, heads, len, d] with contiguous channels")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
+    if t.device != like.device:
+        raise ValueError(f"{name} must be on {like.device}, got {t.device}")
+    B, H, L, d = t.shape
+    if t.numel() == 0:
+        return None, _strides(0, 0, 0)
+    b, h, s = t.stride()[:3]
+    if L > 1 and s == 0:
+        raise ValueError(f"{name}: one row for all tokens (token stride 0) is not supported")
+    # (a dimension of one entry has a stride that says nothing)
+    return t.data_ptr(), _strides(b if B > 1 else H * L * d, h if H > 1 else L * d, s if L > 1 else d)
+
+
+def _vector(t: torch.Tensor, name: str, shape, dtype, like: torch.Tensor):
+    """Pointer of a contiguous tensor of the given shape and type on `like`'s device."""
+    p = _dev(t, name, dtype)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if t.device != like.device:
+        raise ValueError(f"{name} must be on {like.device}, got {t.device}")
+    return p
+
+
+def _on(t: torch.Tensor):
+    """Makes the tensor's device the current one (its current stream is the one a call enqueues on)."""
+    return contextlib.nullcontext() if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+
+
+def _scratch(t, name, nbytes, like):
+    """Pointer and size of a workspace: the caller's, or a new one of nbytes."""
+    if t is None:
+        t = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    elif t.device != like.device:
+        raise ValueError(f"{name} must be on {like.device}, got {t.device}")
+    return t, (_dev(t, name) if t.numel() else None), t.numel() * t.element_size()
+
+
+def _window(q, k, left, right, sinks, chunk, q_start, seq_lens, kv_heads, kv_len):
+    if not isinstance(q, torch.Tensor) or not q.is_cuda:
+        raise TypeError("q must be a GPU tensor (there is no CPU path)")
+    if q.dim() != 4:
+        raise ValueError("q must be [B, heads, len, d]")
+    B, Hq, Lq, d = q.shape
+    w = UsvWindow(B, Hq, kv_heads, Lq, kv_len, d, _dt(q), int(left), int(right), int(sinks), int(chunk),
+                  USV_Q_AT_END if q_start is None else int(q_start))
+    if seq_lens is not None:
+        w.seq_lens = _vector(seq_lens, "seq_lens", (B,), torch.int32, q)
+    return w
+
+
+def _window_of(q, k, v, left, right, sinks, chunk, q_start, seq_lens):
+    """UsvWindow with the strides of q, k, v, and their pointers."""
+    for name, t in (("q", q), ("k", k)):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{name} must be a GPU tensor (there is no CPU path)")
+        if t.dim() != 4:
+            raise ValueError(f"{name} must be [B, heads, len, d]")
+    w = _window(q, k, left, right, sinks, chunk, q_start, seq_lens, k.shape[1], k.shape[2])
+    qp, w.q = _rows(q, "q", q)
+    kp, w.k = _rows(k, "k", q, (q.shape[0], k.shape[1], k.shape[2], q.shape[3]))
+    vp_, w.v = _rows(v, "v", q, k.shape)
+    return w, qp, kp, vp_
+
+
+def window_attn(q, k, v, left, right=0, sinks=0, chunk=1, q_start=None, seq_lens=None, scale=0.0, out=None, lse=None,
+                return_lse=False, workspace=None):
+    """usv_window_attn: attention over a window with sinks.  q [B, Hq, Lq, d], k, v [B, Hkv, Lk, d] (bf16 or fp32, any strides with
+    contiguous channels; Hkv divides Hq) -> out like q (and lse [B, Hq, Lq] fp32 if asked).
+
+    left, right, sinks: chunks of `chunk` positions that a query sees before and after its own, and first ones that stay visible
+    (negative left or right: all).  q_start: position of query row 0; None: the queries are the newest tokens.  seq_lens: int32 [B],
+    tokens of each sequence of a padded batch.  workspace: uint8 scratch of window_workspace_bytes(...); None: one is allocated where
+    the call has a use for one."""
+    w, qp, kp, vp_ = _window_of(q, k, v, left, right, sinks, chunk, q_start, seq_lens)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    op, w.out = _rows(out, "out", q, q.shape)
+    if lse is None and return_lse:
+        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
+    lp = None if lse is None else _vector(lse, "lse", q.shape[:3], torch.float32, q)
+    with _on(q):
+        wp, wn = None, 0
+        need = int(lib().usv_window_workspace_bytes(ctypes.byref(w))) if workspace is None else 0
+        if workspace is not None or need:
+            workspace, wp, wn = _scratch(workspace, "workspace", need, q)
+        _check(lib().usv_window_attn(qp, kp, vp_, ctypes.byref(w), float(scale), op, lp, wp, wn, _stream()))
+    return (out, lse) if return_lse else out
+
+
+def window_attn_backward(q, k, v, out, lse, dout, left, right=0, sinks=0, chunk=1, q_start=None, seq_lens=None, scale=0.0,
+                         dq=None, dk=None, dv=None, workspace=None):
+    """usv_window_attn_backward: gradients (dq, dk, dv) of window_attn, from its inputs, its out and lse, and the gradient of out.
+
+    workspace: uint8 scratch of window_workspace_bytes(..., backward=True); None: one is allocated."""
+    w, qp, kp, vp_ = _window_of(q, k, v, left, right, sinks, chunk, q_start, seq_lens)
+    op, w.out = _rows(out, "out", q, q.shape)
+    lp = _vector(lse, "lse", q.shape[:3], torch.float32, q)
+    g = UsvWindowGrads()
+    dop, g.dout = _rows(dout, "dout", q, q.shape)
+    got = []
+    for name, t, like in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
+        if t is None:
+            t = torch.empty(like.shape, dtype=q.dtype, device=q.device)
+        p, st = _rows(t, name, q, like.shape)
+        setattr(g, name, st)
+        got.append((t, p))
+    with _on(q):
+        need = int(lib().usv_window_backward_workspace_bytes(ctypes.byref(w))) if workspace is None else 0
+        workspace, wp, wn = _scratch(workspace, "workspace", max(need, 16), q)
+        _check(lib().usv_window_attn_backward(qp, kp, vp_, op, lp if lse.numel() else None, dop, ctypes.byref(w), ctypes.byref(g),
+                                              float(scale), *(p for _, p in got), wp, wn, _stream()))
+    return tuple(t for t, _ in got)
+
+
+def window_workspace_bytes(q, k, left, right=0, sinks=0, chunk=1, backward=False) -> int:
+    """Bytes of scratch that window_attn (backward: window_attn_backward) uses for tensors of q's and k's shapes; 0: none."""
+    w = _window(q, k, left, right, sinks, chunk, None, None, k.shape[1], k.shape[2])
+    f = lib().usv_window_backward_workspace_bytes if backward else lib().usv_window_workspace_bytes
+    return int(f(ctypes.byref(w)))
 
 
 class _Binding(types.ModuleType):

@@ -6,6 +6,7 @@
 #include <mutex>
 
 #include "usv_internal.h"
+#include "usv_window.h"
 
 namespace {
 
@@ -122,6 +123,110 @@ usv_status check_merge(const usv_shape* sh, const usv_grid* g, usv::Dims* s, usv
   *N = (int)tokens;
   *r = (int)(tokens - sh->seq_valid);
   return USV_OK;
+}
+
+// One tensor's strides in bytes.  written: its rows must not overlap.
+usv_status check_window_strides(const char* name, const usv_strides& st, int heads, int len, int d, long long esz, bool written, usv::Strides3* out) {
+  long long e[3] = {(long long)heads * len * d, (long long)len * d, (long long)d};
+  if (st.token != 0) e[0] = st.batch, e[1] = st.head, e[2] = st.token;
+  for (int i = 0; i < 3; ++i) {
+    if (e[i] < 0 || e[i] > (1LL << 40)) return fail(USV_ERR_INVALID_ARG, "%s: strides must be in [0, 2^40] elements", name);
+    if ((e[i] * esz) % 16 != 0) return fail(USV_ERR_INVALID_ARG, "%s: strides must be multiples of 16 bytes", name);
+    if (written && len > 0 && e[i] < d && (i < 2 || len > 1)) return fail(USV_ERR_INVALID_ARG, "%s: rows overlap (stride %lld, head_dim %d)", name, e[i], d);
+  }
+  *out = {e[0] * esz, e[1] * esz, e[2] * esz};
+  return USV_OK;
+}
+
+constexpr int kMostTokens = 1 << 30;
+
+// Checks everything in `w` but the strides and fills WindowShape.
+usv_status check_window(const usv_window* w, usv::WindowShape* s) {
+  if (!w) return fail(USV_ERR_INVALID_ARG, "window is NULL");
+  if (w->batch < 1 || w->q_heads < 1 || w->kv_heads < 1) return fail(USV_ERR_INVALID_ARG, "batch and heads must be >= 1");
+  if (w->q_heads % w->kv_heads != 0)
+    return fail(USV_ERR_INVALID_ARG, "kv_heads (%d) must divide q_heads (%d)", w->kv_heads, w->q_heads);
+  if (w->q_len < 0 || w->q_len > kMostTokens || w->kv_len < 0 || w->kv_len > kMostTokens)
+    return fail(USV_ERR_INVALID_ARG, "q_len (%d) and kv_len (%d) must be in [0, 2^30]", w->q_len, w->kv_len);
+  if (w->head_dim != 64 && w->head_dim != 128) return fail(USV_ERR_UNSUPPORTED, "head_dim must be 64 or 128 (got %d)", w->head_dim);
+  if (w->dtype != USV_F32 && w->dtype != USV_BF16) return fail(USV_ERR_UNSUPPORTED, "dtype must be USV_F32 or USV_BF16 (got %d)", w->dtype);
+  if (w->chunk < 1 || w->chunk > kMostTokens) return fail(USV_ERR_INVALID_ARG, "chunk (%d) must be in [1, 2^30]", w->chunk);
+  if (w->left > kMostTokens || w->right > kMostTokens || w->sinks < 0 || w->sinks > kMostTokens)
+    return fail(USV_ERR_INVALID_ARG, "left, right must be at most 2^30 and sinks in [0, 2^30]");
+  if (w->q_start != USV_Q_AT_END && (w->q_start < -kMostTokens || w->q_start > kMostTokens))
+    return fail(USV_ERR_INVALID_ARG, "q_start (%d) must be in [-2^30, 2^30] or USV_Q_AT_END", w->q_start);
+  const long long heads = (long long)w->batch * w->q_heads;
+  if (heads > 65535) return fail(USV_ERR_UNSUPPORTED, "batch * q_heads must be <= 65535");
+  if (heads * ((w->q_len > w->kv_len ? w->q_len : w->kv_len) / usv::kWindowRows + 1) > 0x7fffffffLL / 64)
+    return fail(USV_ERR_UNSUPPORTED, "batch * q_heads * length too large");
+  s->B = w->batch, s->Hq = w->q_heads, s->Hkv = w->kv_heads, s->group = w->q_heads / w->kv_heads;
+  s->Lq = w->q_len, s->Lk = w->kv_len;
+  s->left = w->left < 0 ? -1 : w->left, s->right = w->right < 0 ? -1 : w->right, s->chunk = w->chunk;
+  const long long sink = w->left < 0 ? 0 : (long long)w->sinks * w->chunk;
+  s->sink = sink > w->kv_len ? w->kv_len : (int)sink;
+  s->at_end = w->q_start == USV_Q_AT_END;
+  s->q_start = s->at_end ? 0 : w->q_start;
+  s->lens = w->seq_lens;
+  if (reinterpret_cast<uintptr_t>(w->seq_lens) & 3u) return fail(USV_ERR_INVALID_ARG, "seq_lens is not 4-byte aligned");
+  return USV_OK;
+}
+
+// Keys that a block of `rows` query rows sees at most.
+long long window_most_keys(const usv::WindowShape& s, int rows) {
+  if (s.left < 0 || s.right < 0) return s.Lk;
+  const long long n = s.sink + ((long long)s.left + s.right + 1) * s.chunk + rows + s.chunk;
+  return n < s.Lk ? n : s.Lk;
+}
+
+// Pieces that the key list of a block of rows is shared out in: enough to fill the chip, eight tiles of 64 keys each at least
+// (a piece is a workgroup of its own and 64 fp32 rows through memory).
+int window_splits(const usv::WindowShape& s, int d) {
+  const long long wgs = (long long)((s.Lq + usv::kWindowRows - 1) / usv::kWindowRows) * s.B * s.Hq;
+  const long long slots = d == 128 ? 1024 : 1536, tiles = (window_most_keys(s, usv::kWindowRows) + 63) / 64;
+  if (wgs == 0 || 2 * wgs > slots) return 1;
+  const long long by_slots = slots / wgs, by_tiles = tiles / 8;
+  const long long n = by_slots < by_tiles ? by_slots : by_tiles;
+  return n < 2 ? 1 : n > 256 ? 256 : (int)n;
+}
+size_t window_part_bytes(const usv::WindowShape& s, int d, int splits) {
+  return splits > 1 ? (size_t)splits * s.B * s.Hq * s.Lq * (d + 4) * sizeof(float) : 0;  // (d + 1, kept aligned)
+}
+void window_set_parts(usv::WindowArgs* a, int d, int splits, void* ws) {
+  a->splits = splits;
+  a->part_o = static_cast<float*>(ws);
+  a->part_lse = splits > 1 ? a->part_o + (size_t)splits * a->w.B * a->w.Hq * a->w.Lq * d : nullptr;
+}
+
+// Key blocks of the gradient and the pieces of their lists: as many as fill the chip, and so that no list is far longer than the
+// launch's share per workgroup (blocks of sinks are seen by every row).
+void window_grad_plan(usv::WindowGradArgs* g, int block, int rows_per_tile, int slots) {
+  const usv::WindowShape& s = g->f.w;
+  const long long heads = (long long)s.B * s.Hkv;
+  auto tiles = [&](long long rows) { return (rows + rows_per_tile - 1) / rows_per_tile * s.group; };
+  g->block = block;
+  g->blocks = (s.Lk + block - 1) / block;
+  g->sink_blocks = (s.sink + block - 1) / block;
+  long long reach = s.Lq;
+  if (s.left >= 0 && s.right >= 0) {
+    const long long n = ((long long)s.left + s.right + 1) * s.chunk + block + s.chunk;
+    if (n < reach) reach = n;
+  }
+  const long long longest = tiles(reach), sink_list = tiles(s.Lq);
+  const long long all = heads * (g->sink_blocks * sink_list + (g->blocks - g->sink_blocks) * longest);
+  long long piece = (all + slots - 1) / slots;
+  if (piece < 8) piece = 8;
+  auto parts = [&](long long list) { return list > 2 * piece ? (int)((list + piece - 1) / piece) : 1; };
+  g->sink_parts = parts(sink_list);
+  g->parts = parts(longest);
+}
+size_t window_delta_bytes(const usv::WindowShape& s) { return ((size_t)s.B * s.Hq * s.Lq * sizeof(float) + 255) / 256 * 256; }
+size_t window_partial_bytes(const usv::WindowGradArgs& g, int d) {
+  const size_t heads = (size_t)g.f.w.B * g.f.w.Hkv;
+  const size_t slots = heads * ((g.sink_parts > 1 ? (size_t)g.sink_blocks * g.sink_parts : 0) + (g.parts > 1 ? (size_t)(g.blocks - g.sink_blocks) * g.parts : 0));
+  return slots * 2 * g.block * d * sizeof(float);
+}
+void window_grad_plan_for(usv::WindowGradArgs* g, const usv_window* w) {
+  window_grad_plan(g, 64, 32, 1024);
 }
 
 #define USV_TRY(expr)                    \
@@ -624,6 +729,106 @@ usv_status usv_cube_scatter(const void* cube, const usv_shape* shape, const usv_
   USV_TRY(check_ptr(raster, "raster"));
   return hip_result(usv::launch_cube_move(false, cube, raster, g, s, sb[0], sb[1], sb[2], static_cast<hipStream_t>(stream)),
                     "usv_cube_scatter launch");
+}
+
+size_t usv_window_workspace_bytes(const usv_window* w) {
+  usv::WindowShape s;
+  if (check_window(w, &s) != USV_OK) return 0;
+  return window_part_bytes(s, w->head_dim, window_splits(s, w->head_dim));
+}
+
+usv_status usv_window_attn(const void* q, const void* k, const void* v, const usv_window* w, float scale, void* out,
+                           float* lse, void* ws, size_t ws_bytes, void* stream) {
+  usv::WindowArgs a = {};
+  USV_TRY(check_window(w, &a.w));
+  const int d = w->head_dim;
+  const bool bf16 = w->dtype == USV_BF16;
+  const long long esz = bf16 ? 2 : 4;
+  USV_TRY(check_window_strides("q", w->q, w->q_heads, w->q_len, d, esz, false, &a.sq));
+  USV_TRY(check_window_strides("k", w->k, w->kv_heads, w->kv_len, d, esz, false, &a.sk));
+  USV_TRY(check_window_strides("v", w->v, w->kv_heads, w->kv_len, d, esz, false, &a.sv));
+  USV_TRY(check_window_strides("out", w->out, w->q_heads, w->q_len, d, esz, true, &a.so));
+  if (w->q_len > 0) {
+    USV_TRY(check_ptr(q, "q"));
+    USV_TRY(check_ptr(out, "out"));
+    if (w->kv_len > 0) {
+      USV_TRY(check_ptr(k, "k"));
+      USV_TRY(check_ptr(v, "v"));
+    }
+    if (lse) USV_TRY(check_ptr(lse, "lse"));
+  }
+  if (!(scale <= 0.f) && !std::isfinite(scale)) return fail(USV_ERR_INVALID_ARG, "scale must be finite");
+  int splits = window_splits(a.w, d);
+  if (!ws) splits = 1;
+  else {
+    USV_TRY(check_ptr(ws, "ws"));
+    if (ws_bytes < window_part_bytes(a.w, d, splits))
+      return fail(USV_ERR_WORKSPACE, "ws holds %zu bytes, %zu are needed", ws_bytes, window_part_bytes(a.w, d, splits));
+  }
+  a.q = q, a.k = k, a.v = v, a.out = out, a.lse = lse;
+  a.scale = scale > 0.f ? scale : 1.f / std::sqrt((float)d);
+  window_set_parts(&a, d, splits, ws);
+  if (w->q_len == 0) return hip_result(hipSuccess, "");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  hipError_t e = usv::launch_window_f32(a, bf16, d, st);
+  if (e == hipSuccess && splits > 1) e = usv::launch_window_join(a, bf16, d, st);
+  return hip_result(e, "usv_window_attn");
+}
+
+size_t usv_window_backward_workspace_bytes(const usv_window* w) {
+  usv::WindowGradArgs g = {};
+  if (check_window(w, &g.f.w) != USV_OK) return 0;
+  window_grad_plan_for(&g, w);
+  const size_t n = window_delta_bytes(g.f.w) + window_partial_bytes(g, w->head_dim);
+  return n ? n : 16;
+}
+
+usv_status usv_window_attn_backward(const void* q, const void* k, const void* v, const void* out, const float* lse,
+                                    const void* dout, const usv_window* w, const usv_window_grads* grads, float scale,
+                                    void* dq, void* dk, void* dv, void* ws, size_t ws_bytes, void* stream) {
+  usv::WindowGradArgs g = {};
+  usv::WindowArgs& a = g.f;
+  USV_TRY(check_window(w, &a.w));
+  if (!grads) return fail(USV_ERR_INVALID_ARG, "grads is NULL");
+  const int d = w->head_dim;
+  const bool bf16 = w->dtype == USV_BF16;
+  const long long esz = bf16 ? 2 : 4;
+  USV_TRY(check_window_strides("q", w->q, w->q_heads, w->q_len, d, esz, false, &a.sq));
+  USV_TRY(check_window_strides("k", w->k, w->kv_heads, w->kv_len, d, esz, false, &a.sk));
+  USV_TRY(check_window_strides("v", w->v, w->kv_heads, w->kv_len, d, esz, false, &a.sv));
+  USV_TRY(check_window_strides("out", w->out, w->q_heads, w->q_len, d, esz, false, &a.so));
+  USV_TRY(check_window_strides("dout", grads->dout, w->q_heads, w->q_len, d, esz, false, &g.sdo));
+  USV_TRY(check_window_strides("dq", grads->dq, w->q_heads, w->q_len, d, esz, true, &g.sdq));
+  USV_TRY(check_window_strides("dk", grads->dk, w->kv_heads, w->kv_len, d, esz, true, &g.sdk));
+  USV_TRY(check_window_strides("dv", grads->dv, w->kv_heads, w->kv_len, d, esz, true, &g.sdv));
+  if (w->q_len > 0) {
+    USV_TRY(check_ptr(q, "q"));
+    USV_TRY(check_ptr(out, "out"));
+    USV_TRY(check_ptr(lse, "lse"));
+    USV_TRY(check_ptr(dout, "dout"));
+    USV_TRY(check_ptr(dq, "dq"));
+  }
+  if (w->kv_len > 0) {
+    USV_TRY(check_ptr(k, "k"));
+    USV_TRY(check_ptr(v, "v"));
+    USV_TRY(check_ptr(dk, "dk"));
+    USV_TRY(check_ptr(dv, "dv"));
+  }
+  if (!(scale <= 0.f) && !std::isfinite(scale)) return fail(USV_ERR_INVALID_ARG, "scale must be finite");
+  window_grad_plan_for(&g, w);
+  USV_TRY(check_ptr(ws, "ws"));
+  const size_t need = window_delta_bytes(a.w) + window_partial_bytes(g, d);
+  if (ws_bytes < need) return fail(USV_ERR_WORKSPACE, "ws holds %zu bytes, %zu are needed", ws_bytes, need);
+  a.q = q, a.k = k, a.v = v, a.out = const_cast<void*>(out), a.lse = const_cast<float*>(lse);
+  a.scale = scale > 0.f ? scale : 1.f / std::sqrt((float)d);
+  a.splits = 1;
+  g.dout = dout, g.dq = dq, g.dk = dk, g.dv = dv;
+  g.delta = static_cast<float*>(ws);
+  g.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + window_delta_bytes(a.w));
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  hipError_t e = usv::launch_window_grad_f32(g, bf16, d, st);
+  if (e == hipSuccess && window_partial_bytes(g, d)) e = usv::launch_window_grad_join(g, bf16, d, st);
+  return hip_result(e, "usv_window_attn_backward");
 }
 
 const char* usv_status_string(int32_t status) {

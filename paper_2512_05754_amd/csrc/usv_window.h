@@ -1,0 +1,180 @@
+// Windowed attention with sinks: what its kernels share (who sees whom, key lists, launch arguments).
+//
+// Tokens are grouped in chunks of `chunk` consecutive positions (the frames of a clip, or single tokens).  In a sequence of n tokens
+// the query at position p, 0 <= p < n, of chunk c = p / chunk sees the keys
+//   [lo, hi)  lo = max(0, (c - left) chunk),  hi = min(n, (c + right + 1) chunk)      (left, right < 0: no limit on that side)
+//   and [0, min(sink, hi)),  sink = sinks * chunk.
+// lo and hi grow with p, so the keys of a block of rows are the union of two stretches that follow from its first and its last row.
+// Positions outside [0, n) have no token: such rows see nothing.  A query always sees its own position, so no other row is empty.
+#pragma once
+
+#include "usv_internal.h"
+
+namespace usv {
+
+struct Strides3 {
+  long long batch, head, token;  // bytes
+};
+
+struct WindowShape {
+  int B, Hq, Hkv, group;  // group = Hq / Hkv query heads share a key head
+  int Lq, Lk;
+  int left, right, chunk, sink;  // sink in tokens; 0 where there is no left limit (nothing to add then)
+  int q_start, at_end;           // position of query row 0; at_end: the last row is the sequence's last token
+  const int32_t* lens;           // NULL, or [B] tokens of each sequence
+};
+
+struct WindowArgs {
+  WindowShape w;
+  const void *q, *k, *v;
+  void* out;
+  float* lse;
+  Strides3 sq, sk, sv, so;
+  float scale;
+  int splits;  // > 1: the key list is shared out, results go to part_o [splits][rows][d] (normalised, fp32) and part_lse [splits][rows]
+  float *part_o, *part_lse;
+};
+
+struct WindowGradArgs {
+  WindowArgs f;  // q, k, v, out, lse as the forward pass left them
+  const void* dout;
+  void *dq, *dk, *dv;
+  Strides3 sdo, sdq, sdk, sdv;
+  float* delta;  // [B, Hq, Lq]: sum over the channels of dout * out
+  // Key blocks are `block` keys.  Those below sink_blocks (every later row sees them) have sink_parts pieces, the others parts.
+  int block, blocks, sink_blocks, sink_parts, parts;
+  float* partial;  // dk, dv of the pieces: [slot][2][block][d]; a block in one piece has no slot
+};
+
+struct WindowSeq {
+  int n, first;  // tokens, position of query row 0
+};
+__host__ __device__ inline WindowSeq window_seq(const WindowShape& w, int n) {
+  n = n < 0 ? 0 : n > w.Lk ? w.Lk : n;
+  return {n, w.at_end ? n - w.Lq : w.q_start};
+}
+__device__ __forceinline__ WindowSeq window_seq_of(const WindowShape& w, int b) {
+  return window_seq(w, w.lens ? __builtin_amdgcn_readfirstlane(w.lens[b]) : w.Lk);
+}
+
+struct WindowRange {
+  int lo, hi;
+};
+__host__ __device__ inline WindowRange window_range(const WindowShape& w, int n, int p) {
+  if (p < 0 || p >= n) return {0, 0};
+  const int c = p / w.chunk;
+  const long long end = ((long long)c + w.right + 1) * w.chunk, begin = ((long long)c - w.left) * w.chunk;
+  WindowRange r;
+  r.hi = w.right < 0 || end > n ? n : (int)end;
+  r.lo = w.left < 0 || begin < 0 ? 0 : (int)begin;
+  return r;
+}
+__host__ __device__ inline bool window_sees(const WindowRange& r, int sink, int j) { return j < r.hi && (j >= r.lo || j < sink); }
+
+// Keys of the rows [blk * rows, + rows), sinks ahead of the window: entry i of the list is key i where i < head, else i + skip.
+struct WindowKeys {
+  int i0, i1;       // rows of the block that hold a token (i0 >= i1: none)
+  int head, skip, count;
+  int all_hi, all_lo, all_sink;  // every row sees the keys [all_lo, all_hi) and [0, all_sink)
+};
+__host__ __device__ inline WindowKeys window_keys(const WindowShape& w, const WindowSeq& s, int blk, int rows) {
+  WindowKeys k;
+  const long long r0 = (long long)blk * rows;
+  long long i0 = -(long long)s.first, i1 = (long long)s.n - s.first;
+  if (i0 < r0) i0 = r0;
+  if (i1 > r0 + rows) i1 = r0 + rows;
+  if (i1 > w.Lq) i1 = w.Lq;
+  k.i0 = (int)i0, k.i1 = (int)(i1 < i0 ? i0 : i1);
+  k.head = k.skip = k.count = k.all_hi = k.all_lo = k.all_sink = 0;
+  if (i0 >= i1) return k;
+  const WindowRange a = window_range(w, s.n, s.first + k.i0), z = window_range(w, s.n, s.first + k.i1 - 1);
+  const int sink = w.sink < z.hi ? w.sink : z.hi;
+  if (a.lo > sink) k.head = sink, k.skip = a.lo - sink;  // (else the two stretches meet: one from 0 on)
+  k.count = z.hi - k.skip;
+  k.all_hi = a.hi, k.all_lo = z.lo, k.all_sink = w.sink < a.hi ? w.sink : a.hi;
+  return k;
+}
+// Whether every row sees all the entries [t, t + tile).
+__host__ __device__ inline bool window_tile_open(const WindowKeys& k, int t, int tile) {
+  if (t + tile > k.count) return false;
+  if (t + tile <= k.head) return t + tile <= k.all_sink;
+  if (t < k.head) return false;
+  const int first = t + k.skip, end = first + tile;
+  return end <= k.all_hi && (first >= k.all_lo || end <= k.all_sink);
+}
+__host__ __device__ inline int window_key(const WindowKeys& k, int i) { return i < k.head ? i : i + k.skip; }
+
+// Query rows [i0, i1) of one head that see a key of [k0, k0 + block).
+struct WindowRows {
+  int i0, i1;
+};
+__host__ __device__ inline WindowRows window_rows(const WindowShape& w, const WindowSeq& s, int k0, int block) {
+  if (k0 >= s.n) return {0, 0};
+  const long long k1 = (long long)k0 + block < s.n ? (long long)k0 + block : s.n;
+  long long p0 = 0, p1 = s.n;
+  if (w.right >= 0) p0 = ((long long)k0 / w.chunk - w.right) * w.chunk;
+  if (w.left >= 0 && k0 >= w.sink) p1 = ((k1 - 1) / w.chunk + w.left + 1) * w.chunk;
+  if (p0 < 0) p0 = 0;
+  if (p1 > s.n) p1 = s.n;
+  long long i0 = p0 - s.first, i1 = p1 - s.first;
+  if (i0 < 0) i0 = 0;
+  if (i1 > w.Lq) i1 = w.Lq;
+  if (i0 >= i1) return {0, 0};
+  return {(int)i0, (int)i1};
+}
+
+// Launch slot -> (block of rows, head).  Later blocks of rows see more keys (up to the window), so the launch begins with them; the
+// heads are spread over the XCDs, the query heads of one key head on the same one as far as the numbers allow.
+struct WindowSlot {
+  int blk, b, h;
+};
+__device__ __forceinline__ WindowSlot window_slot(const WindowShape& w, int slot, int blocks) {
+  const int heads = w.B * w.Hq;
+  const int blk = blocks - 1 - slot / heads;
+  const int r = slot % heads;
+  int bh = r;
+  if (heads % kNumXcd == 0) {  // slots go round the XCDs: XCD x gets heads / 8 neighbouring heads
+    const int per = heads / kNumXcd;
+    bh = (r % kNumXcd) * per + r / kNumXcd;
+  }
+  return {blk, bh / w.Hq, bh % w.Hq};
+}
+
+// Gradient of the keys: launch slot -> (key block, piece of its list of rows, head).  Blocks that every row sees come first, in pieces of
+// their own number; a block in one piece writes its result itself, the others write sums for the join (slot).
+struct WindowPiece {
+  int block, part, parts, b, h;
+  long long slot;
+};
+__host__ __device__ inline long long window_piece_slot(const WindowGradArgs& g, int bh, int block, int part) {
+  const long long heads = (long long)g.f.w.B * g.f.w.Hkv;
+  if (block < g.sink_blocks) return ((long long)block * g.sink_parts + part) * heads + bh;
+  const long long before = g.sink_parts > 1 ? g.sink_blocks * (long long)g.sink_parts : 0;
+  return (before + (block - g.sink_blocks) * (long long)g.parts + part) * heads + bh;
+}
+__host__ __device__ inline unsigned window_pieces(const WindowGradArgs& g) {
+  return (unsigned)(((long long)g.sink_blocks * g.sink_parts + (long long)(g.blocks - g.sink_blocks) * g.parts) * g.f.w.B * g.f.w.Hkv);
+}
+__device__ __forceinline__ WindowPiece window_piece(const WindowGradArgs& g, int slot) {
+  const int heads = g.f.w.B * g.f.w.Hkv;
+  WindowPiece p;
+  int y = slot / heads, bh = slot % heads;
+  if (heads % kNumXcd == 0) bh = (bh % kNumXcd) * (heads / kNumXcd) + bh / kNumXcd;
+  const bool sink = y < g.sink_blocks * g.sink_parts;
+  if (!sink) y -= g.sink_blocks * g.sink_parts;
+  p.parts = sink ? g.sink_parts : g.parts;
+  p.block = (sink ? 0 : g.sink_blocks) + y / p.parts;
+  p.part = y % p.parts;
+  p.b = bh / g.f.w.Hkv, p.h = bh % g.f.w.Hkv;
+  p.slot = p.parts > 1 ? window_piece_slot(g, bh, p.block, p.part) : -1;
+  return p;
+}
+
+constexpr int kWindowRows = 64;  // query rows of a workgroup
+
+hipError_t launch_window_f32(const WindowArgs& a, bool bf16, int d, hipStream_t st);
+hipError_t launch_window_join(const WindowArgs& a, bool bf16, int d, hipStream_t st);
+hipError_t launch_window_grad_f32(const WindowGradArgs& a, bool bf16, int d, hipStream_t st);
+hipError_t launch_window_grad_join(const WindowGradArgs& a, bool bf16, int d, hipStream_t st);
+
+}  // namespace usv

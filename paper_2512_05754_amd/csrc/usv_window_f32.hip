@@ -1,0 +1,419 @@
+// Windowed attention with sinks on the fp32 matrix cores: forward, gradient of the queries, gradients of the keys and values, and the
+// kernels that join pieces.
+//
+// Forward: one workgroup = 4 waves = 64 query rows of one head, 16 rows a wave; key tiles of 32 rows go through LDS, the next one is
+// in registers while the present one is multiplied.  v_mfma_f32_16x16x4_f32 on the transposes (lane = (c, G), c = lane % 16, G =
+// lane / 16; A holds row c and contraction slot G, B column c and slot G, the result column c and rows 4 G .. 4 G + 3):
+//   S^T = K Q^T     slot G of step (u, e): channel 16 u + 4 G + e, so a lane reads four steps at once
+//   O^T += V^T P^T  slot G of step (m, r): key 16 m + 4 G + r, where the accumulators of S^T hold it: P^T needs no move
+// so a lane column is a query, its statistics stay in four lanes, and every product is an fp32 one.
+//
+// Gradients, with P = exp(scale S - lse), D = sum over the channels of dout * out, dS = P (dP - D), dP = dout V^T:
+//   dQ = scale dS K    a workgroup per 64 query rows, as the forward pass (S^T and dP^T, then dQ^T += K^T dS^T)
+//   dV = P^T dout, dK = scale dS^T Q    a workgroup per 64 keys (16 a wave) that walks the rows that see them, all query heads of the
+//     key head in turn: S and dP with the keys as columns, then dV^T += dout^T P and dK^T += Q^T dS
+// P and dS are formed twice and nothing is added with atomics, so a call repeats its bits.  Rows that hold no token are never
+// contracted over: row and key indices are clamped to ones that some partner sees, and the mask takes the doubles out.
+//
+// What bounds it: the fp32 matrix cores (154 TFLOP/s in an 8192-cubed product).
+#include "usv_attn_bf16.h"
+#include "usv_window.h"
+
+namespace usv {
+namespace {
+
+constexpr int kTile = 32;  // keys (key gradient: query rows) of a step
+
+__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 load4(const uint16_t* p) {
+  const uint2 x = *reinterpret_cast<const uint2*>(p);
+  return bf16_pair(x.x, x.y);
+}
+template <typename T>
+__device__ __forceinline__ void put4(void* p, const float4& x) {
+  store4<std::is_same<T, float>::value>(p, x, 0);
+}
+template <typename T>
+__device__ __forceinline__ const T* row_of(const void* base, const Strides3& s, int b, int h, long long row) {
+  return reinterpret_cast<const T*>(static_cast<const unsigned char*>(base) + b * s.batch + h * s.head + row * s.token);
+}
+template <typename T>
+__device__ __forceinline__ T* row_of(void* base, const Strides3& s, int b, int h, long long row) {
+  return reinterpret_cast<T*>(static_cast<unsigned char*>(base) + b * s.batch + h * s.head + row * s.token);
+}
+__device__ __forceinline__ float at(const float4& x, int e) { return e == 0 ? x.x : e == 1 ? x.y : e == 2 ? x.z : x.w; }
+__device__ __forceinline__ f32x4 mfma(float a, float b, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+// A tile of kTile rows of two tensors, on its way to LDS: thread t holds channels 4 (t % 8) + 32 x of row t / 8.
+template <typename T, int D>
+struct Pair {
+  static constexpr int X = D / 32, PITCH = D + 4;
+  float4 a[X], b[X];
+  __device__ __forceinline__ void load(const T* ra, const T* rb) {
+    const int c = 4 * (threadIdx.x & 7);
+#pragma unroll
+    for (int x = 0; x < X; ++x) a[x] = load4(ra + c + 32 * x), b[x] = load4(rb + c + 32 * x);
+  }
+  __device__ __forceinline__ void store(float* la, float* lb) const {
+    const int at = (threadIdx.x >> 3) * PITCH + 4 * (threadIdx.x & 7);
+#pragma unroll
+    for (int x = 0; x < X; ++x) {
+      *reinterpret_cast<float4*>(la + at + 32 * x) = a[x];
+      *reinterpret_cast<float4*>(lb + at + 32 * x) = b[x];
+    }
+  }
+};
+
+// Rows of 16 columns: s[m] += rows 16 m + .. of the tile times the lane's column held in f (channels 16 u + 4 G + e).
+template <int D>
+__device__ __forceinline__ void rows_times(const float* tile, const float4 (&f)[D / 16], f32x4 (&s)[2]) {
+  const int c = threadIdx.x & 15, G = (threadIdx.x >> 4) & 3;
+#pragma unroll
+  for (int u = 0; u < D / 16; ++u)
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const float4 x = *reinterpret_cast<const float4*>(tile + (16 * m + c) * (D + 4) + 16 * u + 4 * G);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[m] = mfma(at(x, e), at(f[u], e), s[m]);
+    }
+}
+// o (channels x columns) += tile^T (channels x its 32 rows) times p (the rows as the accumulators hold them)
+template <int D>
+__device__ __forceinline__ void columns_times(const float* tile, const f32x4 (&p)[2], f32x4 (&o)[D / 16]) {
+  const int c = threadIdx.x & 15, G = (threadIdx.x >> 4) & 3;
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) o[dt] = mfma(tile[(16 * m + 4 * G + r) * (D + 4) + 16 * dt + c], p[m][r], o[dt]);
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void window_fwd(WindowArgs a) {
+  __shared__ __attribute__((aligned(16))) float sk[kTile * (D + 4)], sv[kTile * (D + 4)];
+  const int blocks = (a.w.Lq + kWindowRows - 1) / kWindowRows;
+  const WindowSlot at_ = window_slot(a.w, blockIdx.x, blocks);
+  const int hk = at_.h / a.w.group;
+  const WindowSeq seq = window_seq_of(a.w, at_.b);
+  const WindowKeys keys = window_keys(a.w, seq, at_.blk, kWindowRows);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, G = lane >> 4;
+  const int row = at_.blk * kWindowRows + 16 * wave + c;
+  const bool live = row >= keys.i0 && row < keys.i1;
+  const int tiles = (keys.count + kTile - 1) / kTile;
+  const int t0 = (int)((long long)tiles * blockIdx.y / a.splits), t1 = (int)((long long)tiles * (blockIdx.y + 1) / a.splits);
+
+  f32x4 o[D / 16];
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;  // of the scaled logits in the log2 domain; l: this lane's share
+  const float sl = a.scale * kLog2e;
+  if (t0 < t1) {
+    const int qrow = min(max(row, keys.i0), keys.i1 - 1);
+    const WindowRange range = window_range(a.w, seq.n, seq.first + qrow);
+    float4 qf[D / 16];
+    const T* qp = row_of<T>(a.q, a.sq, at_.b, at_.h, qrow) + 4 * G;
+#pragma unroll
+    for (int u = 0; u < D / 16; ++u) qf[u] = load4(qp + 16 * u);
+    Pair<T, D> next;
+    auto fetch = [&](int t) {
+      const long long key = window_key(keys, min(t * kTile + (int)(threadIdx.x >> 3), keys.count - 1));
+      next.load(row_of<T>(a.k, a.sk, at_.b, hk, key), row_of<T>(a.v, a.sv, at_.b, hk, key));
+    };
+    fetch(t0);
+    for (int t = t0; t < t1; ++t) {
+      __syncthreads();
+      next.store(sk, sv);
+      __syncthreads();
+      if (t + 1 < t1) fetch(t + 1);
+      f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      rows_times<D>(sk, qf, s);
+      if (!window_tile_open(keys, t * kTile, kTile)) {
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int i = t * kTile + 16 * mt + 4 * G + r;
+            const bool sees = i < keys.count && window_sees(range, a.w.sink, window_key(keys, i));
+            s[mt][r] = sees ? s[mt][r] : -INFINITY;
+          }
+      }
+      float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+      mx = fmaxf(m, max_over_groups(mx) * sl);
+      const float ref = mx == -INFINITY ? 0.f : mx;
+      const float alpha = fast_exp2(m - ref);
+      m = mx;
+      l *= alpha;
+      f32x4 p[2];
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          p[mt][r] = fast_exp2(fmaf(s[mt][r], sl, -ref));
+          l += p[mt][r];
+        }
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) o[dt] *= alpha;
+      columns_times<D>(sv, p, o);
+    }
+  }
+  l = sum_over_groups(l);
+  if (row >= a.w.Lq) return;
+  const bool some = live && l > 0.f;
+  const float inv = some ? 1.f / l : 0.f;
+  const float lse = some ? (m + __log2f(l)) * kLn2 : -INFINITY;
+  const long long rows = (long long)a.w.B * a.w.Hq * a.w.Lq, id = ((long long)at_.b * a.w.Hq + at_.h) * a.w.Lq + row;
+  const bool parts = a.splits > 1;
+  unsigned char* dst = parts ? reinterpret_cast<unsigned char*>(a.part_o + (blockIdx.y * rows + id) * D)
+                             : reinterpret_cast<unsigned char*>(row_of<T>(a.out, a.so, at_.b, at_.h, row));
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) {
+    const float4 x = some ? make_float4(o[dt][0] * inv, o[dt][1] * inv, o[dt][2] * inv, o[dt][3] * inv) : make_float4(0.f, 0.f, 0.f, 0.f);
+    if (parts) put4<float>(dst + (16 * dt + 4 * G) * 4, x);
+    else put4<T>(dst + (16 * dt + 4 * G) * sizeof(T), x);
+  }
+  if (G == 0) {
+    if (parts) a.part_lse[blockIdx.y * rows + id] = lse;
+    else if (a.lse) a.lse[id] = lse;
+  }
+}
+
+// out = sum of the pieces, each weighed with its share exp(lse_piece - lse).  One wave per 256 / D ... rows: D / 4 lanes a row.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void window_join(WindowArgs a) {
+  const long long rows = (long long)a.w.B * a.w.Hq * a.w.Lq;
+  const long long id = (long long)blockIdx.x * (1024 / D) + threadIdx.x / (D / 4);
+  if (id >= rows) return;
+  const int ch = 4 * (threadIdx.x % (D / 4));
+  float m = -INFINITY;
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_lse[s * rows + id]);
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float l = 0.f;
+  if (m != -INFINITY) {
+    for (int s = 0; s < a.splits; ++s) {
+      const float w = fast_exp2((a.part_lse[s * rows + id] - m) * kLog2e);
+      if (w == 0.f) continue;  // (a piece without keys)
+      const float4 x = load4(a.part_o + (s * rows + id) * D + ch);
+      l += w;
+      acc.x = fmaf(w, x.x, acc.x), acc.y = fmaf(w, x.y, acc.y), acc.z = fmaf(w, x.z, acc.z), acc.w = fmaf(w, x.w, acc.w);
+    }
+    const float inv = 1.f / l;
+    acc.x *= inv, acc.y *= inv, acc.z *= inv, acc.w *= inv;
+  }
+  const int row = (int)(id % a.w.Lq), bh = (int)(id / a.w.Lq);
+  put4<T>(row_of<T>(a.out, a.so, bh / a.w.Hq, bh % a.w.Hq, row) + ch, acc);
+  if (a.lse && ch == 0) a.lse[id] = m == -INFINITY ? -INFINITY : m + __log2f(l) * kLn2;
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void window_grad_q(WindowGradArgs g) {
+  const WindowArgs& a = g.f;
+  __shared__ __attribute__((aligned(16))) float sk[kTile * (D + 4)], sv[kTile * (D + 4)];
+  const int blocks = (a.w.Lq + kWindowRows - 1) / kWindowRows;
+  const WindowSlot at_ = window_slot(a.w, blockIdx.x, blocks);
+  const int hk = at_.h / a.w.group;
+  const WindowSeq seq = window_seq_of(a.w, at_.b);
+  const WindowKeys keys = window_keys(a.w, seq, at_.blk, kWindowRows);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, G = lane >> 4;
+  const int row = at_.blk * kWindowRows + 16 * wave + c;
+  const bool live = row >= keys.i0 && row < keys.i1;
+  const int tiles = (keys.count + kTile - 1) / kTile;
+  const long long id = ((long long)at_.b * a.w.Hq + at_.h) * a.w.Lq + row;
+  f32x4 dq[D / 16];
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) dq[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (tiles > 0) {
+    const int qrow = min(max(row, keys.i0), keys.i1 - 1);
+    const WindowRange range = window_range(a.w, seq.n, seq.first + qrow);
+    float4 qf[D / 16], dof[D / 16];
+    const T* qp = row_of<T>(a.q, a.sq, at_.b, at_.h, qrow) + 4 * G;
+    const T* dop = row_of<T>(g.dout, g.sdo, at_.b, at_.h, qrow) + 4 * G;
+    const T* op = row_of<T>(static_cast<const void*>(a.out), a.so, at_.b, at_.h, qrow) + 4 * G;
+    float delta = 0.f;
+#pragma unroll
+    for (int u = 0; u < D / 16; ++u) {
+      qf[u] = load4(qp + 16 * u);
+      dof[u] = load4(dop + 16 * u);
+      const float4 of = load4(op + 16 * u);
+      delta += dof[u].x * of.x + dof[u].y * of.y + dof[u].z * of.z + dof[u].w * of.w;
+    }
+    delta = sum_over_groups(delta);
+    if (G == 0 && live) g.delta[id] = delta;
+    const float sl = a.scale * kLog2e, ref = a.lse[((long long)at_.b * a.w.Hq + at_.h) * a.w.Lq + qrow] * kLog2e;
+    Pair<T, D> next;
+    auto fetch = [&](int t) {
+      const long long key = window_key(keys, min(t * kTile + (int)(threadIdx.x >> 3), keys.count - 1));
+      next.load(row_of<T>(a.k, a.sk, at_.b, hk, key), row_of<T>(a.v, a.sv, at_.b, hk, key));
+    };
+    fetch(0);
+    for (int t = 0; t < tiles; ++t) {
+      __syncthreads();
+      next.store(sk, sv);
+      __syncthreads();
+      if (t + 1 < tiles) fetch(t + 1);
+      f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, dp[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      rows_times<D>(sk, qf, s);
+      rows_times<D>(sv, dof, dp);
+      const bool open = window_tile_open(keys, t * kTile, kTile);
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int i = t * kTile + 16 * mt + 4 * G + r;
+          const bool sees = open || (i < keys.count && window_sees(range, a.w.sink, window_key(keys, i)));
+          s[mt][r] = sees ? fast_exp2(fmaf(s[mt][r], sl, -ref)) * (dp[mt][r] - delta) : 0.f;
+        }
+      columns_times<D>(sk, s, dq);
+    }
+  }
+  if (row >= a.w.Lq) return;
+  T* dst = row_of<T>(g.dq, g.sdq, at_.b, at_.h, row);
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) {
+    const float4 x = live ? make_float4(dq[dt][0] * a.scale, dq[dt][1] * a.scale, dq[dt][2] * a.scale, dq[dt][3] * a.scale) : make_float4(0.f, 0.f, 0.f, 0.f);
+    put4<T>(dst + 16 * dt + 4 * G, x);
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void window_grad_kv(WindowGradArgs g) {
+  const WindowArgs& a = g.f;
+  constexpr int KB = 64;
+  __shared__ __attribute__((aligned(16))) float sq[kTile * (D + 4)], sdo[kTile * (D + 4)];
+  __shared__ __attribute__((aligned(16))) float4 srow[kTile];  // log-sum-exp (log2 domain), D, lo, hi of a row
+  const WindowPiece pc = window_piece(g, blockIdx.x);
+  const int k0 = pc.block * KB;
+  const WindowSeq seq = window_seq_of(a.w, pc.b);
+  const WindowRows rows = window_rows(a.w, seq, k0, KB);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, G = lane >> 4;
+  const int key = k0 + 16 * wave + c;
+  f32x4 dk[D / 16], dv[D / 16];
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) dk[dt] = dv[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int tiles = (rows.i1 - rows.i0 + kTile - 1) / kTile;
+  const long long all = (long long)tiles * a.w.group;
+  const int n0 = (int)(all * pc.part / pc.parts), n1 = (int)(all * (pc.part + 1) / pc.parts);
+  if (n0 < n1) {
+    const int krow = min(key, seq.n - 1);
+    float4 kf[D / 16], vf[D / 16];
+    const T* kp = row_of<T>(a.k, a.sk, pc.b, pc.h, krow) + 4 * G;
+    const T* vp = row_of<T>(a.v, a.sv, pc.b, pc.h, krow) + 4 * G;
+#pragma unroll
+    for (int u = 0; u < D / 16; ++u) kf[u] = load4(kp + 16 * u), vf[u] = load4(vp + 16 * u);
+    const float sl = a.scale * kLog2e;
+    Pair<T, D> next;
+    float4 next_row = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto fetch = [&](int n) {
+      const int h = pc.h * a.w.group + n / tiles, i = rows.i0 + (n % tiles) * kTile + (int)(threadIdx.x >> 3);
+      const int row = min(i, rows.i1 - 1);
+      next.load(row_of<T>(a.q, a.sq, pc.b, h, row), row_of<T>(g.dout, g.sdo, pc.b, h, row));
+      if ((threadIdx.x & 7) == 0) {
+        const long long id = ((long long)pc.b * a.w.Hq + h) * a.w.Lq + row;
+        const WindowRange r = i < rows.i1 ? window_range(a.w, seq.n, seq.first + i) : WindowRange{0, 0};
+        next_row = make_float4(a.lse[id] * kLog2e, g.delta[id], __int_as_float(r.lo), __int_as_float(r.hi));
+      }
+    };
+    fetch(n0);
+    for (int n = n0; n < n1; ++n) {
+      __syncthreads();
+      next.store(sq, sdo);
+      if ((threadIdx.x & 7) == 0) srow[threadIdx.x >> 3] = next_row;
+      __syncthreads();
+      if (n + 1 < n1) fetch(n + 1);
+      f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, dp[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      rows_times<D>(sq, kf, s);
+      rows_times<D>(sdo, vf, dp);
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float4 x = srow[16 * mt + 4 * G + r];
+          const WindowRange range = {__float_as_int(x.z), __float_as_int(x.w)};
+          const bool sees = window_sees(range, a.w.sink < range.hi ? a.w.sink : range.hi, key);
+          const float p = sees ? fast_exp2(fmaf(s[mt][r], sl, -x.x)) : 0.f;
+          s[mt][r] = p;
+          dp[mt][r] = sees ? p * (dp[mt][r] - x.y) : 0.f;
+        }
+      columns_times<D>(sdo, s, dv);
+      columns_times<D>(sq, dp, dk);
+    }
+  }
+  if (pc.slot >= 0) {
+    float* dst = g.partial + pc.slot * (2LL * KB * D) + (16 * wave + c) * D + 4 * G;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) {
+      put4<float>(dst + 16 * dt, make_float4(dk[dt][0], dk[dt][1], dk[dt][2], dk[dt][3]));
+      put4<float>(dst + KB * D + 16 * dt, make_float4(dv[dt][0], dv[dt][1], dv[dt][2], dv[dt][3]));
+    }
+  } else if (key < a.w.Lk) {
+    T* pk = row_of<T>(g.dk, g.sdk, pc.b, pc.h, key) + 4 * G;
+    T* pv = row_of<T>(g.dv, g.sdv, pc.b, pc.h, key) + 4 * G;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) {
+      put4<T>(pk + 16 * dt, make_float4(dk[dt][0] * a.scale, dk[dt][1] * a.scale, dk[dt][2] * a.scale, dk[dt][3] * a.scale));
+      put4<T>(pv + 16 * dt, make_float4(dv[dt][0], dv[dt][1], dv[dt][2], dv[dt][3]));
+    }
+  }
+}
+
+// dk, dv of a block = sum of its pieces, in their order.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void window_grad_join(WindowGradArgs g) {
+  const WindowArgs& a = g.f;
+  const int heads = a.w.B * a.w.Hkv, split_blocks = g.parts > 1 ? g.blocks : g.sink_blocks;
+  const int rows_per = 1024 / D;  // rows of a workgroup
+  const int bh = blockIdx.x % heads, x = blockIdx.x / heads;
+  const int block = x / (g.block / rows_per), sub = x % (g.block / rows_per);
+  if (block >= split_blocks) return;
+  const int parts = block < g.sink_blocks ? g.sink_parts : g.parts;
+  if (parts <= 1) return;
+  const int r = sub * rows_per + threadIdx.x / (D / 4), ch = 4 * (threadIdx.x % (D / 4));
+  const int key = block * g.block + r;
+  if (key >= a.w.Lk) return;
+  float4 dk = make_float4(0.f, 0.f, 0.f, 0.f), dv = dk;
+  for (int p = 0; p < parts; ++p) {
+    const float* src = g.partial + window_piece_slot(g, bh, block, p) * (2LL * g.block * D) + r * D + ch;
+    const float4 u = load4(src), v = load4(src + g.block * D);
+    dk.x += u.x, dk.y += u.y, dk.z += u.z, dk.w += u.w;
+    dv.x += v.x, dv.y += v.y, dv.z += v.z, dv.w += v.w;
+  }
+  const int b = bh / a.w.Hkv, h = bh % a.w.Hkv;
+  put4<T>(row_of<T>(g.dk, g.sdk, b, h, key) + ch, make_float4(dk.x * a.scale, dk.y * a.scale, dk.z * a.scale, dk.w * a.scale));
+  put4<T>(row_of<T>(g.dv, g.sdv, b, h, key) + ch, dv);
+}
+
+template <typename F>
+hipError_t by_type(bool bf16, int d, F f) {
+  if (bf16) d == 128 ? f(uint16_t{}, std::integral_constant<int, 128>{}) : f(uint16_t{}, std::integral_constant<int, 64>{});
+  else d == 128 ? f(float{}, std::integral_constant<int, 128>{}) : f(float{}, std::integral_constant<int, 64>{});
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_window_f32(const WindowArgs& a, bool bf16, int d, hipStream_t st) {
+  const dim3 grid((unsigned)((a.w.Lq + kWindowRows - 1) / kWindowRows * a.w.B * a.w.Hq), a.splits);
+  return by_type(bf16, d, [&](auto t, auto dc) { window_fwd<decltype(t), decltype(dc)::value><<<grid, 256, 0, st>>>(a); });
+}
+
+hipError_t launch_window_join(const WindowArgs& a, bool bf16, int d, hipStream_t st) {
+  const long long rows = (long long)a.w.B * a.w.Hq * a.w.Lq, per = 1024 / d;
+  return by_type(bf16, d, [&](auto t, auto dc) { window_join<decltype(t), decltype(dc)::value><<<(unsigned)((rows + per - 1) / per), 256, 0, st>>>(a); });
+}
+
+hipError_t launch_window_grad_f32(const WindowGradArgs& g, bool bf16, int d, hipStream_t st) {
+  const unsigned q_grid = (unsigned)((g.f.w.Lq + kWindowRows - 1) / kWindowRows * g.f.w.B * g.f.w.Hq);
+  return by_type(bf16, d, [&](auto t, auto dc) {
+    constexpr int D = decltype(dc)::value;
+    if (q_grid) window_grad_q<decltype(t), D><<<q_grid, 256, 0, st>>>(g);
+    if (g.blocks) window_grad_kv<decltype(t), D><<<window_pieces(g), 256, 0, st>>>(g);
+  });
+}
+
+hipError_t launch_window_grad_join(const WindowGradArgs& g, bool bf16, int d, hipStream_t st) {
+  const int split_blocks = g.parts > 1 ? g.blocks : g.sink_blocks;
+  const unsigned grid = (unsigned)(g.f.w.B * g.f.w.Hkv * split_blocks * (g.block / (1024 / d)));
+  return by_type(bf16, d, [&](auto t, auto dc) { window_grad_join<decltype(t), decltype(dc)::value><<<grid, 256, 0, st>>>(g); });
+}
+
+}  // namespace usv
