@@ -586,6 +586,62 @@ usv_status usv_window_attn_backward(const void* q, const void* k, const void* v,
                                     const void* dout, const usv_window* w, const usv_window_grads* grads, float scale,
                                     void* dq, void* dk, void* dv, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * A key/value cache in 4 or 8 bits, in pages, for generation frame after frame (or token after token): rows are quantised
+ * as they are written, read back, or attended to where they lie.
+ * A page holds page_size consecutive positions of one sequence; page_table[b][p / page_size] names the page of position p
+ * of sequence b.  32 neighbouring channels of a row share a scale 2^e; a value x is held as the code nearest to x / 2^e
+ * (ties to even):
+ *   bits = 4  e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives;  e = the least of -125 .. 125 with max|x| <= 7 * 2^e
+ *   bits = 8  e4m3: up to 448;                                       e = the least of -117 .. 119 with max|x| <= 464 * 2^e
+ * (beyond the last e, from 2.9e38 on, the largest code is held).
+ * A group that holds an infinity or a NaN reads back as NaN.
+ * The buffer: per page and key head, in this order, the K codes [page_size][d * bits / 8] (4 bits: two to a byte, the even
+ * channel in the low half), the V codes, the K scales [page_size][d / 32] (byte e + 127; 255 = NaN), the V scales.  Its contents need no
+ * preparation: positions that were never written must not be read.
+ */
+typedef struct {
+  int32_t batch;       /* sequences, >= 1 */
+  int32_t kv_heads;    /* >= 1 */
+  int32_t head_dim;    /* 64 or 128 */
+  int32_t bits;        /* 4 or 8 */
+  int32_t page_size;   /* a multiple of 16, at most 65536 */
+  int32_t pages;       /* pages of the buffer, >= 1 */
+  int32_t table_pages; /* entries of a sequence in page_table, >= 1; table_pages * page_size <= 2^30 */
+  const int32_t* page_table; /* device [batch, table_pages] */
+} usv_cache;
+
+/* Bytes of the buffer (page_table and batch are not used).  0 for an invalid `c`. */
+size_t usv_cache_bytes(const usv_cache* c);
+
+/* Writes row i < rows of sequence b to position starts[b] + i.
+ * k, v   : [batch, kv_heads, rows, d] of dtype (device, read only), element strides k_strides, v_strides (NULL =
+ *          contiguous; as those of usv_window)
+ * starts : device int32 [batch];  counts : NULL, or device int32 [batch]: only rows i < counts[b] are written
+ * Rows at positions outside the table, or whose page id lies outside [0, pages), are not written.  Two rows of one call
+ * that name the same place leave one of the two, or a mixture, there. */
+usv_status usv_cache_write(void* cache, const usv_cache* c, const void* k, const void* v, int32_t dtype, int32_t rows,
+                           const usv_strides* k_strides, const usv_strides* v_strides, const int32_t* starts,
+                           const int32_t* counts, void* stream);
+
+/* The values held at positions starts[b] + i, i < rows, in dtype (exact in both).  Arguments as above; k, v are written.
+ * Rows i >= counts[b] are left as they were; rows outside the table or of a page id outside [0, pages) are written as 0. */
+usv_status usv_cache_read(const void* cache, const usv_cache* c, void* k, void* v, int32_t dtype, int32_t rows,
+                          const usv_strides* k_strides, const usv_strides* v_strides, const int32_t* starts,
+                          const int32_t* counts, void* stream);
+
+/* Bytes of device scratch usv_cache_attn uses: 0 where the rows fill the chip (and for invalid arguments). */
+size_t usv_cache_attn_workspace_bytes(const usv_cache* c, const usv_window* w);
+
+/* usv_window_attn of the newest w->q_len tokens of every sequence over its cached keys and values (their own rows have been
+ * written before).  Of `w`: batch, kv_heads and head_dim agree with `c`; kv_len <= table_pages * page_size bounds the
+ * lengths; q_start = USV_Q_AT_END; seq_lens is required; dtype = USV_BF16 (USV_ERR_UNSUPPORTED otherwise); the strides of k
+ * and v are not used.  Only positions that some query sees are read, and only their table entries; page ids outside
+ * [0, pages) are clamped into range, so no memory outside the buffer is touched, but the rows that see such a page hold
+ * unspecified values.  out, lse, scale, ws as usv_window_attn; the products are those of the values the cache holds. */
+usv_status usv_cache_attn(const void* q, const void* cache, const usv_cache* c, const usv_window* w, float scale, void* out,
+                          float* lse, void* ws, size_t ws_bytes, void* stream);
+
 /* Static string for a status code. */
 const char* usv_status_string(int32_t status);
 

@@ -89,3 +89,51 @@ def window_attn_backward(Q, K, V, out, dout, M, scale=None):
             ek[b, g][some] += terms.T @ np.abs(q)
             mv[b, g][some] += P.T @ np.abs(do)
     return (dq, dk, dv), (mq, mk, mv), (eq, ek, np.zeros(K.shape))
+
+
+E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+E4M3 = np.array([m * 2.0 ** -9 if e == 0 else (8 + m) * 2.0 ** (e - 10) for e in range(16) for m in range(8)][:-1])  # (the last code is NaN)
+
+
+def code_values(bits):
+    """The value of every code of 4 or 8 bits."""
+    if bits == 4:
+        return np.concatenate([E2M1, -E2M1])
+    one = np.append(E4M3, np.nan)
+    return np.concatenate([one, -one])
+
+
+def cache_values(X, bits):
+    """What the cache holds of X [..., d]: per group of 32 channels the least scale 2^e at which the largest value lies no more than half a
+    step beyond the largest code, and the nearest code (of two equally near ones the one of even number)."""
+    X = np.asarray(X, dtype=np.float64)
+    codes, border, least, last = (E2M1, 7.0, -125, 125) if bits == 4 else (E4M3, 464.0, -117, 119)
+    g = X.reshape(-1, 32)
+    out = np.full(g.shape, np.nan)
+    for i, row in enumerate(g):
+        if not np.isfinite(row).all():
+            continue
+        top = np.abs(row).max()
+        e = least
+        if top > 0:
+            e = min(last, max(least, math.ceil(math.log2(top / border)) - 2))
+            while top > border * 2.0 ** e and e < last:
+                e += 1
+        y = np.abs(row) / 2.0 ** e
+        hi = np.clip(np.searchsorted(codes, y), 1, len(codes) - 1)
+        lo = hi - 1
+        near_hi = (codes[hi] - y < y - codes[lo]) | ((codes[hi] - y == y - codes[lo]) & (hi % 2 == 0))
+        out[i] = np.copysign(np.where(near_hi, codes[hi], codes[lo]), row) * 2.0 ** e
+    return out.reshape(X.shape)
+
+
+def cache_decode(buf, page, row, head, which, page_size, d, bits):
+    """The row of K (which 0) or V (1) that a cache buffer [pages, heads, bytes] holds at a place, from its bytes."""
+    cb, sb = d * bits // 8, d // 32
+    b = buf[page, head]
+    codes = b[which * page_size * cb + row * cb:][:cb]
+    scales = b[2 * page_size * cb + which * page_size * sb + row * sb:][:sb].astype(np.int64)
+    if bits == 4:
+        codes = np.stack([codes & 15, codes >> 4], -1).reshape(-1)
+    x = code_values(bits)[codes].reshape(-1, 32) * 2.0 ** (scales[:, None] - 127.0)
+    return np.where(scales[:, None] == 255, np.nan, x).reshape(-1)

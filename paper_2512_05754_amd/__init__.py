@@ -30,6 +30,11 @@ _BINDING_NAMES = (
     "window_attn",
     "window_attn_backward",
     "window_workspace_bytes",
+    "cache_empty",
+    "cache_write",
+    "cache_read",
+    "cache_attn",
+    "cache_attn_workspace_bytes",
     "workspace_bytes",
     "lib",
     "lib_path",

@@ -58,6 +58,11 @@ EXPORTED_SYMBOLS = (
     "usv_window_attn",
     "usv_window_backward_workspace_bytes",
     "usv_window_attn_backward",
+    "usv_cache_bytes",
+    "usv_cache_write",
+    "usv_cache_read",
+    "usv_cache_attn_workspace_bytes",
+    "usv_cache_attn",
     "usv_status_string",
     "usv_last_error",
 )
@@ -105,6 +110,11 @@ class UsvWindow(ctypes.Structure):
 
 class UsvWindowGrads(ctypes.Structure):
     _fields_ = [(n, UsvStrides) for n in ("dout", "dq", "dk", "dv")]
+
+
+class UsvCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "kv_heads", "head_dim", "bits", "page_size", "pages", "table_pages")]
+    _fields_ += [("page_table", ctypes.c_void_p)]
 
 
 def lib_path() -> str:
@@ -212,6 +222,12 @@ def lib() -> ctypes.CDLL:
     L.usv_window_backward_workspace_bytes.restype, L.usv_window_backward_workspace_bytes.argtypes = sz, [wp]
     L.usv_window_attn_backward.restype = i32
     L.usv_window_attn_backward.argtypes = [vp, vp, vp, vp, vp, vp, wp, ctypes.POINTER(UsvWindowGrads), f32, vp, vp, vp, vp, sz, vp]
+    cp = ctypes.POINTER(UsvCache)
+    L.usv_cache_bytes.restype, L.usv_cache_bytes.argtypes = sz, [cp]
+    L.usv_cache_write.restype, L.usv_cache_write.argtypes = i32, [vp, cp, vp, vp, i32, i32, stp, stp, vp, vp, vp]
+    L.usv_cache_read.restype, L.usv_cache_read.argtypes = i32, [vp, cp, vp, vp, i32, i32, stp, stp, vp, vp, vp]
+    L.usv_cache_attn_workspace_bytes.restype, L.usv_cache_attn_workspace_bytes.argtypes = sz, [cp, wp]
+    L.usv_cache_attn.restype, L.usv_cache_attn.argtypes = i32, [vp, vp, cp, wp, f32, vp, vp, vp, sz, vp]
     L.usv_status_string.restype, L.usv_status_string.argtypes = ctypes.c_char_p, [i32]
     L.usv_last_error.restype, L.usv_last_error.argtypes = ctypes.c_char_p, []
     if calls is not None:
@@ -814,7 +830,7 @@ def _scratch(t, name, nbytes, like):
     return t, (_dev(t, name) if t.numel() else None), t.numel() * t.element_size()
 
 
-def _window(q, k, left, right, sinks, chunk, q_start, seq_lens, kv_heads, kv_len):
+def _window(q, left, right, sinks, chunk, q_start, seq_lens, kv_heads, kv_len):
     if not isinstance(q, torch.Tensor) or not q.is_cuda:
         raise TypeError("q must be a GPU tensor (there is no CPU path)")
     if q.dim() != 4:
@@ -834,7 +850,7 @@ def _window_of(q, k, v, left, right, sinks, chunk, q_start, seq_lens):
             raise TypeError(f"{name} must be a GPU tensor (there is no CPU path)")
         if t.dim() != 4:
             raise ValueError(f"{name} must be [B, heads, len, d]")
-    w = _window(q, k, left, right, sinks, chunk, q_start, seq_lens, k.shape[1], k.shape[2])
+    w = _window(q, left, right, sinks, chunk, q_start, seq_lens, k.shape[1], k.shape[2])
     qp, w.q = _rows(q, "q", q)
     kp, w.k = _rows(k, "k", q, (q.shape[0], k.shape[1], k.shape[2], q.shape[3]))
     vp_, w.v = _rows(v, "v", q, k.shape)
@@ -893,9 +909,117 @@ def window_attn_backward(q, k, v, out, lse, dout, left, right=0, sinks=0, chunk=
 
 def window_workspace_bytes(q, k, left, right=0, sinks=0, chunk=1, backward=False) -> int:
     """Bytes of scratch that window_attn (backward: window_attn_backward) uses for tensors of q's and k's shapes; 0: none."""
-    w = _window(q, k, left, right, sinks, chunk, None, None, k.shape[1], k.shape[2])
+    w = _window(q, left, right, sinks, chunk, None, None, k.shape[1], k.shape[2])
     f = lib().usv_window_backward_workspace_bytes if backward else lib().usv_window_workspace_bytes
     return int(f(ctypes.byref(w)))
+
+
+def cache_empty(pages, kv_heads, page_size, head_dim, bits=4, device="cuda:0"):
+    """A cache of `pages` pages of page_size positions: uint8 [pages, kv_heads, bytes], uninitialised."""
+    c = UsvCache(1, int(kv_heads), int(head_dim), int(bits), int(page_size), int(pages), 1, None)
+    n = int(lib().usv_cache_bytes(ctypes.byref(c)))
+    if n == 0:
+        raise ValueError(lib().usv_last_error().decode())
+    return torch.empty((int(pages), int(kv_heads), n // (int(pages) * int(kv_heads))), dtype=torch.uint8, device=device)
+
+
+def _cache(cache, page_table, head_dim, bits):
+    """UsvCache of a cache tensor and a page table, and the tensor's pointer."""
+    p = _dev(cache, "cache", torch.uint8)
+    if cache.dim() != 3:
+        raise ValueError("cache must be [pages, kv_heads, bytes] (cache_empty)")
+    tp = _dev(page_table, "page_table", torch.int32)
+    if page_table.dim() != 2 or page_table.device != cache.device:
+        raise ValueError("page_table must be [B, pages of a sequence] on the cache's device")
+    per = 2 * (head_dim * int(bits) // 8 + head_dim // 32)  # bytes of a position: codes and scales of K and V
+    if per <= 0 or cache.shape[2] % per != 0:
+        raise ValueError(f"a page of {cache.shape[2]} bytes does not hold rows of {head_dim} channels in {bits} bits")
+    return UsvCache(page_table.shape[0], cache.shape[1], head_dim, int(bits), cache.shape[2] // per, cache.shape[0], page_table.shape[1], tp), p
+
+
+def _cache_rows(cache, k, v, page_table, starts, counts, bits):
+    c, p = _cache(cache, page_table, k.shape[3], bits)
+    B, H, n, d = k.shape
+    if B != c.batch or H != c.kv_heads:
+        raise ValueError(f"k must be [{c.batch}, {c.kv_heads}, rows, d], got {list(k.shape)}")
+    if k.device != cache.device:
+        raise ValueError(f"k must be on {cache.device}, got {k.device}")
+    kp, ks = _rows(k, "k", k)
+    vp_, vs = _rows(v, "v", k, k.shape)
+    sp = _vector(starts, "starts", (B,), torch.int32, k)
+    np_ = None if counts is None else _vector(counts, "counts", (B,), torch.int32, k)
+    return p, c, kp, vp_, n, ks, vs, sp, np_
+
+
+def cache_write(cache, k, v, page_table, starts, bits=4, counts=None):
+    """usv_cache_write: quantises rows k, v [B, Hkv, n, d] (bf16 or fp32, any strides with contiguous channels) into the cache, row i of
+    sequence b at position starts[b] + i.  page_table int32 [B, pages of a sequence]; starts, counts int32 [B] (counts: rows that count)."""
+    for name, t in (("k", k), ("v", v)):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{name} must be a GPU tensor (there is no CPU path)")
+        if t.dim() != 4:
+            raise ValueError(f"{name} must be [B, heads, rows, d]")
+    p, c, kp, vp_, n, ks, vs, sp, np_ = _cache_rows(cache, k, v, page_table, starts, counts, bits)
+    with _on(k):
+        _check(lib().usv_cache_write(p, ctypes.byref(c), kp, vp_, _dt(k), n, ctypes.byref(ks), ctypes.byref(vs), sp, np_, _stream()))
+    return cache
+
+
+def cache_read(cache, page_table, starts, rows, head_dim=128, bits=4, counts=None, dtype=torch.bfloat16, k=None, v=None):
+    """usv_cache_read: the values held at positions starts[b] + i, i < rows -> k, v [B, Hkv, rows, d] of dtype (or into the given k, v)."""
+    if not isinstance(cache, torch.Tensor) or cache.dim() != 3 or not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise ValueError("cache must be [pages, kv_heads, bytes] and page_table [B, pages of a sequence]")
+    shape = (page_table.shape[0], cache.shape[1], int(rows), int(head_dim))
+    if k is None:
+        k = torch.empty(shape, dtype=dtype if v is None else v.dtype, device=cache.device)
+    if v is None:
+        v = torch.empty(shape, dtype=k.dtype, device=cache.device)
+    if tuple(k.shape) != shape:
+        raise ValueError(f"k must be {list(shape)}, got {list(k.shape)}")
+    p, c, kp, vp_, n, ks, vs, sp, np_ = _cache_rows(cache, k, v, page_table, starts, counts, bits)
+    with _on(k):
+        _check(lib().usv_cache_read(p, ctypes.byref(c), kp, vp_, _dt(k), n, ctypes.byref(ks), ctypes.byref(vs), sp, np_, _stream()))
+    return k, v
+
+
+def _cache_window(q, cache, page_table, seq_lens, left, right, sinks, chunk, bits):
+    if not isinstance(q, torch.Tensor) or not q.is_cuda:
+        raise TypeError("q must be a GPU tensor (there is no CPU path)")
+    if q.dim() != 4:
+        raise ValueError("q must be [B, heads, len, d]")
+    c, p = _cache(cache, page_table, q.shape[3], bits)
+    if cache.device != q.device:
+        raise ValueError(f"cache must be on {q.device}, got {cache.device}")
+    return c, p, _window(q, left, right, sinks, chunk, None, seq_lens, c.kv_heads, c.table_pages * c.page_size)
+
+
+def cache_attn(q, cache, page_table, seq_lens, left=-1, right=0, sinks=0, chunk=1, bits=4, scale=0.0, out=None, lse=None,
+               return_lse=False, workspace=None):
+    """usv_cache_attn: window_attn of the newest tokens q [B, Hq, Lq, d] (bf16) over the cached keys and values of their sequences.
+
+    seq_lens int32 [B]: tokens of each sequence in the cache, the queries' own included; left, right, sinks, chunk as window_attn.
+    workspace: uint8 scratch of cache_attn_workspace_bytes(...); None: one is allocated where the call has a use for one."""
+    c, p, w = _cache_window(q, cache, page_table, seq_lens, left, right, sinks, chunk, bits)
+    qp, w.q = _rows(q, "q", q)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    op, w.out = _rows(out, "out", q, q.shape)
+    if lse is None and return_lse:
+        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
+    lp = None if lse is None else _vector(lse, "lse", q.shape[:3], torch.float32, q)
+    with _on(q):
+        wp, wn = None, 0
+        need = int(lib().usv_cache_attn_workspace_bytes(ctypes.byref(c), ctypes.byref(w))) if workspace is None else 0
+        if workspace is not None or need:
+            workspace, wp, wn = _scratch(workspace, "workspace", need, q)
+        _check(lib().usv_cache_attn(qp, p, ctypes.byref(c), ctypes.byref(w), float(scale), op, lp, wp, wn, _stream()))
+    return (out, lse) if return_lse else out
+
+
+def cache_attn_workspace_bytes(q, cache, page_table, left=-1, right=0, sinks=0, chunk=1, bits=4) -> int:
+    """Bytes of scratch that cache_attn uses for these tensors' shapes; 0: none."""
+    c, _, w = _cache_window(q, cache, page_table, None, left, right, sinks, chunk, bits)
+    return int(lib().usv_cache_attn_workspace_bytes(ctypes.byref(c), ctypes.byref(w)))
 
 
 class _Binding(types.ModuleType):

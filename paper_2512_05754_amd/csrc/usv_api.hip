@@ -6,7 +6,7 @@
 #include <mutex>
 
 #include "usv_internal.h"
-#include "usv_window.h"
+#include "usv_cache.h"
 
 namespace {
 
@@ -227,6 +227,64 @@ size_t window_partial_bytes(const usv::WindowGradArgs& g, int d) {
 }
 void window_grad_plan_for(usv::WindowGradArgs* g, const usv_window* w) {
   window_grad_plan(g, 64, 32, 1024);
+}
+
+usv_status check_cache(const usv_cache* c, usv::CacheShape* s) {
+  if (!c) return fail(USV_ERR_INVALID_ARG, "cache shape is NULL");
+  if (c->batch < 1 || c->kv_heads < 1) return fail(USV_ERR_INVALID_ARG, "batch and kv_heads must be >= 1");
+  if ((long long)c->batch * c->kv_heads > 65535) return fail(USV_ERR_UNSUPPORTED, "batch * kv_heads must be <= 65535");
+  if (c->head_dim != 64 && c->head_dim != 128) return fail(USV_ERR_UNSUPPORTED, "head_dim must be 64 or 128 (got %d)", c->head_dim);
+  if (c->bits != 4 && c->bits != 8) return fail(USV_ERR_UNSUPPORTED, "bits must be 4 or 8 (got %d)", c->bits);
+  if (c->page_size < 16 || c->page_size > 65536 || c->page_size % usv::kCacheGroup != 0)
+    return fail(USV_ERR_INVALID_ARG, "page_size (%d) must be a multiple of 16 in [16, 65536]", c->page_size);
+  if (c->pages < 1) return fail(USV_ERR_INVALID_ARG, "pages must be >= 1");
+  if (c->table_pages < 1 || (long long)c->table_pages * c->page_size > kMostTokens)
+    return fail(USV_ERR_INVALID_ARG, "table_pages (%d) must be >= 1 and cover at most 2^30 positions", c->table_pages);
+  *s = usv::CacheShape{c->batch, c->kv_heads, c->head_dim, c->bits, c->page_size, c->pages, c->table_pages, c->page_table};
+  return USV_OK;
+}
+
+usv_status check_cache_rows(const void* cache, const usv_cache* c, const void* k, const void* v, int32_t dtype, int32_t rows,
+                            const usv_strides* ks, const usv_strides* vs, const int32_t* starts, bool written, usv::CacheRowsArgs* a) {
+  const usv_status st = check_cache(c, &a->c);
+  if (st != USV_OK) return st;
+  if (dtype != USV_F32 && dtype != USV_BF16) return fail(USV_ERR_UNSUPPORTED, "dtype must be USV_F32 or USV_BF16 (got %d)", dtype);
+  if (rows < 0 || rows > kMostTokens || (long long)rows * c->batch * c->kv_heads > (1LL << 34))
+    return fail(USV_ERR_INVALID_ARG, "rows (%d) must be in [0, 2^30] and batch * kv_heads * rows at most 2^34", rows);
+  const usv_strides none = {0, 0, 0};
+  const long long esz = dtype == USV_BF16 ? 2 : 4;
+  usv_status bad = check_window_strides("k", ks ? *ks : none, c->kv_heads, rows, c->head_dim, esz, written, &a->sk);
+  if (bad == USV_OK) bad = check_window_strides("v", vs ? *vs : none, c->kv_heads, rows, c->head_dim, esz, written, &a->sv);
+  if (bad == USV_OK && rows > 0) bad = check_ptr(k, "k");
+  if (bad == USV_OK && rows > 0) bad = check_ptr(v, "v");
+  if (bad == USV_OK) bad = check_ptr(cache, "cache");
+  if (bad == USV_OK) bad = check_ptr(c->page_table, "page_table");
+  if (bad == USV_OK) bad = check_ptr(starts, "starts");
+  return bad;
+}
+
+// cache_attn: what `w` has to be besides a valid window.
+usv_status check_cache_attn(const usv_cache* c, const usv_window* w, usv::CacheShape* s, usv::WindowShape* ws) {
+  usv_status st = check_cache(c, s);
+  if (st == USV_OK) st = check_window(w, ws);
+  if (st != USV_OK) return st;
+  if (w->dtype != USV_BF16) return fail(USV_ERR_UNSUPPORTED, "usv_cache_attn takes bf16 queries only");
+  if (w->batch != c->batch || w->kv_heads != c->kv_heads || w->head_dim != c->head_dim)
+    return fail(USV_ERR_INVALID_ARG, "batch, kv_heads and head_dim of the window and the cache differ");
+  if (w->kv_len > (long long)c->table_pages * c->page_size)
+    return fail(USV_ERR_INVALID_ARG, "kv_len (%d) is beyond the table's positions", w->kv_len);
+  if (w->q_start != USV_Q_AT_END) return fail(USV_ERR_INVALID_ARG, "q_start must be USV_Q_AT_END");
+  if ((long long)w->q_len * ws->group > kMostTokens) return fail(USV_ERR_UNSUPPORTED, "too many query rows");
+  return USV_OK;
+}
+// Pieces of the key list: enough workgroups to fill the chip several times over (sequences differ in length), 512 keys each at least.
+int cache_attn_splits(const usv::WindowShape& s) {
+  const int rows = usv::cache_attn_rows(s);
+  const long long all = (long long)s.Lq * s.group, wgs = (all + rows - 1) / rows * s.B * s.Hkv;
+  const long long target = rows == 16 ? 2048 : 512, by_keys = window_most_keys(s, rows) / 512;
+  if (wgs == 0 || 2 * wgs > target) return 1;
+  const long long by_wgs = target / wgs, n = by_wgs < by_keys ? by_wgs : by_keys;
+  return n < 2 ? 1 : n > 256 ? 256 : (int)n;
 }
 
 #define USV_TRY(expr)                    \
@@ -829,6 +887,79 @@ usv_status usv_window_attn_backward(const void* q, const void* k, const void* v,
   hipError_t e = usv::launch_window_grad_f32(g, bf16, d, st);
   if (e == hipSuccess && window_partial_bytes(g, d)) e = usv::launch_window_grad_join(g, bf16, d, st);
   return hip_result(e, "usv_window_attn_backward");
+}
+
+size_t usv_cache_bytes(const usv_cache* c) {
+  usv::CacheShape s;
+  if (check_cache(c, &s) != USV_OK) return 0;
+  return (size_t)s.pages * s.H * s.head_bytes();
+}
+
+usv_status usv_cache_write(void* cache, const usv_cache* c, const void* k, const void* v, int32_t dtype, int32_t rows,
+                           const usv_strides* k_strides, const usv_strides* v_strides, const int32_t* starts,
+                           const int32_t* counts, void* stream) {
+  usv::CacheRowsArgs a = {};
+  USV_TRY(check_cache_rows(cache, c, k, v, dtype, rows, k_strides, v_strides, starts, false, &a));
+  if (counts) USV_TRY(check_ptr(counts, "counts"));
+  a.cache = static_cast<unsigned char*>(cache);
+  a.starts = starts, a.counts = counts, a.rows = rows;
+  a.k = const_cast<void*>(k), a.v = const_cast<void*>(v);
+  if (rows == 0) return hip_result(hipSuccess, "");
+  return hip_result(usv::launch_cache_write(a, dtype == USV_BF16, static_cast<hipStream_t>(stream)), "usv_cache_write");
+}
+
+usv_status usv_cache_read(const void* cache, const usv_cache* c, void* k, void* v, int32_t dtype, int32_t rows,
+                          const usv_strides* k_strides, const usv_strides* v_strides, const int32_t* starts,
+                          const int32_t* counts, void* stream) {
+  usv::CacheRowsArgs a = {};
+  USV_TRY(check_cache_rows(cache, c, k, v, dtype, rows, k_strides, v_strides, starts, true, &a));
+  if (counts) USV_TRY(check_ptr(counts, "counts"));
+  a.cache = const_cast<unsigned char*>(static_cast<const unsigned char*>(cache));
+  a.starts = starts, a.counts = counts, a.rows = rows;
+  a.k = k, a.v = v;
+  if (rows == 0) return hip_result(hipSuccess, "");
+  return hip_result(usv::launch_cache_read(a, dtype == USV_BF16, static_cast<hipStream_t>(stream)), "usv_cache_read");
+}
+
+size_t usv_cache_attn_workspace_bytes(const usv_cache* c, const usv_window* w) {
+  usv::CacheShape s;
+  usv::WindowShape ws;
+  if (check_cache_attn(c, w, &s, &ws) != USV_OK) return 0;
+  return window_part_bytes(ws, s.d, cache_attn_splits(ws));
+}
+
+usv_status usv_cache_attn(const void* q, const void* cache, const usv_cache* c, const usv_window* w, float scale, void* out,
+                          float* lse, void* ws, size_t ws_bytes, void* stream) {
+  usv::CacheAttnArgs a = {};
+  USV_TRY(check_cache_attn(c, w, &a.c, &a.f.w));
+  const int d = a.c.d;
+  USV_TRY(check_window_strides("q", w->q, w->q_heads, w->q_len, d, 2, false, &a.f.sq));
+  USV_TRY(check_window_strides("out", w->out, w->q_heads, w->q_len, d, 2, true, &a.f.so));
+  USV_TRY(check_ptr(cache, "cache"));
+  USV_TRY(check_ptr(c->page_table, "page_table"));
+  if (!w->seq_lens) return fail(USV_ERR_INVALID_ARG, "seq_lens is NULL");
+  if (w->q_len > 0) {
+    USV_TRY(check_ptr(q, "q"));
+    USV_TRY(check_ptr(out, "out"));
+    if (lse) USV_TRY(check_ptr(lse, "lse"));
+  }
+  if (!(scale <= 0.f) && !std::isfinite(scale)) return fail(USV_ERR_INVALID_ARG, "scale must be finite");
+  int splits = cache_attn_splits(a.f.w);
+  if (!ws) splits = 1;
+  else {
+    USV_TRY(check_ptr(ws, "ws"));
+    if (ws_bytes < window_part_bytes(a.f.w, d, splits))
+      return fail(USV_ERR_WORKSPACE, "ws holds %zu bytes, %zu are needed", ws_bytes, window_part_bytes(a.f.w, d, splits));
+  }
+  a.cache = static_cast<const unsigned char*>(cache);
+  a.f.q = q, a.f.out = out, a.f.lse = lse;
+  a.f.scale = scale > 0.f ? scale : 1.f / std::sqrt((float)d);
+  window_set_parts(&a.f, d, splits, ws);
+  if (w->q_len == 0) return hip_result(hipSuccess, "");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  hipError_t e = usv::launch_cache_attn(a, st);
+  if (e == hipSuccess && splits > 1) e = usv::launch_window_join(a.f, true, d, st);
+  return hip_result(e, "usv_cache_attn");
 }
 
 const char* usv_status_string(int32_t status) {

@@ -1,0 +1,310 @@
+// cache_attn: attention of the newest tokens of every sequence over its quantised, paged keys and values.
+//
+// One workgroup = 4 waves = one key head of one sequence, ROWS = 16 NT rows (query tokens x the query heads that share the key head; NT = 1
+// or 4) and a stretch of the keys; a wave takes every fourth step of 32 keys (two groups of 16, each within a page, so that a page
+// is looked up with scalar instructions) with an online softmax of its own, and the four are merged at the end.  With few rows the keys are also shared out
+// over workgroups, whose pieces window_join joins.
+//
+// Matrix cores (v_mfma_f32_16x16x32_bf16, lane = (c, G), c = lane % 16, G = lane / 16), on the transposes:
+//   S^T = K Q^T: lane (c, G) has key c of a group and the channels D / 4 * G ..: one contiguous load whose codes share one scale.  Which channels
+//     a contraction slot stands for is free as long as Q agrees.  v_cvt_scalef32_pk_bf16_* turns two codes into two bf16 under the scale
+//     in one instruction, exactly, so the products are those of the values that the codes stand for.
+//   O^T += V^T P^T: V is loaded and converted the same way, laid down in LDS (the wave's own 32 rows, no barrier) and read back
+//     column by column with ds_read_b64_tr_b16; P^T is what the accumulators of S^T hold.
+// The weights are rounded to bf16 for the second product; their sum is taken unrounded in fp32.
+#include "usv_attn_bf16.h"
+#include "usv_cache.h"
+
+namespace usv {
+namespace {
+
+constexpr float kNoKey = 3.4028234e38f;  // reference of a row that has seen no key yet
+
+template <int D, int BITS>
+struct Raw {  // one lane's share of a key (or value) row
+  static constexpr int WORDS = D / 4 * BITS / 32;
+  unsigned w[WORDS];
+  unsigned scale;
+  __device__ __forceinline__ void load(const unsigned char* codes, const unsigned char* scales) {
+    if constexpr (WORDS == 2) {
+      const uint2 x = *reinterpret_cast<const uint2*>(codes);
+      w[0] = x.x, w[1] = x.y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < WORDS / 4; ++i) {
+        const uint4 x = reinterpret_cast<const uint4*>(codes)[i];
+        w[4 * i] = x.x, w[4 * i + 1] = x.y, w[4 * i + 2] = x.z, w[4 * i + 3] = x.w;
+      }
+    }
+    scale = *scales;
+  }
+  __device__ __forceinline__ float factor() const { return __uint_as_float(scale == 255 ? 0x7fc00000u : scale << 23); }
+  // channels 8 t .. 8 t + 7 of the share
+  __device__ __forceinline__ bf16x8 eight(int t, float f) const {
+    typedef __attribute__((__vector_size__(4 * sizeof(unsigned)))) unsigned u32x4;
+    u32x4 r;
+    if constexpr (BITS == 4) {
+      r[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[t], f, 0));
+      r[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[t], f, 1));
+      r[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[t], f, 2));
+      r[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[t], f, 3));
+    } else {
+      r[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * t], f, false));
+      r[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * t], f, true));
+      r[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * t + 1], f, false));
+      r[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * t + 1], f, true));
+    }
+    return __builtin_bit_cast(bf16x8, r);
+  }
+};
+
+template <int D, int BITS, int NT>
+__global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void cache_attn(CacheAttnArgs a, int row_tiles) {
+  constexpr int ROWS = 16 * NT, KS = D / 32, DT = D / 16, OT = DT / 4, CB = D * BITS / 8, SB = D / 32;
+  constexpr int PITCH = D * 2 + 16, AREA = 32 * PITCH, OPITCH = D + 4;
+  static_assert(16 * OPITCH * 4 <= AREA, "a wave's result of 16 rows fits where its V rows were");
+  __shared__ __attribute__((aligned(16))) unsigned char smem[4 * AREA];
+  __shared__ int2 srange[ROWS];
+  __shared__ float sref[4][ROWS], ssum[4][ROWS];
+  const WindowShape& w = a.f.w;
+  const int lane = threadIdx.x & 63, c = lane & 15, G = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tile = blockIdx.x % row_tiles, bh = blockIdx.x / row_tiles, b = bh / w.Hkv, hk = bh % w.Hkv;
+  const WindowSeq seq = window_seq_of(w, b);
+  const int all_rows = w.Lq * w.group, row0 = tile * ROWS, row1 = min(row0 + ROWS, all_rows);
+  const int i0 = row0 / w.group, i1 = (row1 - 1) / w.group + 1;  // query tokens
+  const WindowKeys keys = window_keys(w, seq, i0, i1 - i0);
+  // groups of 16 keys: list entry x is group x where x < head_groups, else x + skip_groups
+  const int lo = keys.head + keys.skip, hi = keys.count + keys.skip;
+  const int head_groups = (keys.head + kCacheGroup - 1) / kCacheGroup;
+  const int skip_groups = max(0, lo / kCacheGroup - head_groups);
+  const int groups = keys.count > 0 ? (hi + kCacheGroup - 1) / kCacheGroup - skip_groups : 0;
+  const int steps = (groups + 1) / 2;
+  const int s0 = (int)((long long)steps * blockIdx.y / a.f.splits), s1 = (int)((long long)steps * (blockIdx.y + 1) / a.f.splits);
+
+  for (int r = threadIdx.x; r < ROWS; r += 256) {
+    const WindowRange x = row0 + r < row1 ? window_range(w, seq.n, seq.first + (row0 + r) / w.group) : WindowRange{0, 0};
+    srange[r] = make_int2(x.lo, x.hi);
+  }
+  bf16x8 qf[NT][KS];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int row = min(row0 + 16 * nt + c, row1 - 1), i = row / w.group, h = hk * w.group + row % w.group;
+    const uint16_t* p = reinterpret_cast<const uint16_t*>(static_cast<const unsigned char*>(a.f.q) + b * a.f.sq.batch + h * a.f.sq.head + i * a.f.sq.token) + D / 4 * G;
+#pragma unroll
+    for (int t = 0; t < KS; ++t) qf[nt][t] = *reinterpret_cast<const bf16x8*>(p + 8 * t);
+  }
+  f32x16 o[NT][OT];
+  float nm[NT], l[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    nm[nt] = kNoKey, l[nt] = 0.f;
+#pragma unroll
+    for (int x = 0; x < OT; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[nt][x][r] = 0.f;
+  }
+  __syncthreads();
+
+  const float sl = a.f.scale * kLog2e;
+  const int page_groups = a.c.page_size / kCacheGroup;
+  const long long head_bytes = a.c.head_bytes();
+  const int32_t* table = a.c.table + (long long)b * a.c.table_pages;
+  unsigned char* const area = smem + wave * AREA;
+  Raw<D, BITS> kr[2], vr[2];
+  auto group_of = [&](int x) { return x < head_groups ? x : x + skip_groups; };
+  // The rows of a group that no row of the workgroup sees are not touched: their lanes take one that is seen.
+  auto fetch = [&](int step) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const int g = group_of(min(2 * step + m, groups - 1));
+      const int slot = g / page_groups, first = (g - slot * page_groups) * kCacheGroup;
+      const int page = min(max(__builtin_amdgcn_readfirstlane(table[slot]), 0), a.c.pages - 1);
+      const unsigned char* base = a.cache + ((long long)page * w.Hkv + hk) * head_bytes;
+      const int j = g * kCacheGroup + c, some = g < head_groups ? g * kCacheGroup : max(g * kCacheGroup, lo);
+      const bool seen = j < hi && (j < keys.head || j >= lo);
+      const int row = first + (seen ? c : some - g * kCacheGroup);
+      const unsigned char* codes = base + (long long)row * CB + CB / 4 * G;
+      const unsigned char* scales = base + 2LL * a.c.page_size * CB + row * SB + (D == 128 ? G : G >> 1);
+      kr[m].load(codes, scales);
+      vr[m].load(codes + (long long)a.c.page_size * CB, scales + a.c.page_size * SB);
+    }
+  };
+  int step = s0 + wave;
+  if (step < s1) fetch(step);
+  for (; step < s1; step += 4) {
+    bf16x8 kf[2][KS];
+    bf16x8 vf[2][KS];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const float fk = kr[m].factor(), fv = vr[m].factor();
+#pragma unroll
+      for (int t = 0; t < KS; ++t) kf[m][t] = kr[m].eight(t, fk), vf[m][t] = vr[m].eight(t, fv);
+    }
+    if (step + 4 < s1) fetch(step + 4);
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int t = 0; t < KS; ++t) *reinterpret_cast<bf16x8*>(area + (16 * m + c) * PITCH + (D / 4 * G + 8 * t) * 2) = vf[m][t];
+    // ---- S^T: s[m][4 nt + r]: key 16 m + 4 G + r of the step, row 16 nt + c
+    float s[2][4 * NT];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int t = 0; t < KS; ++t) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[m][t], qf[nt][t], x, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[m][4 * nt + r] = x[r];
+      }
+    bool open = true;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const int x = 2 * step + m, j0 = group_of(x) * kCacheGroup, j1 = j0 + kCacheGroup;
+      open = open && x < groups && j1 <= keys.all_hi && (j0 >= keys.all_lo || j1 <= keys.all_sink);
+    }
+    if (!open) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int2 rr = srange[16 * nt + c];
+        const WindowRange range = {rr.x, rr.y};
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          const int x = 2 * step + m, j0 = group_of(x) * kCacheGroup + 4 * G;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s[m][4 * nt + r] = x < groups && window_sees(range, w.sink, j0 + r) ? s[m][4 * nt + r] : -INFINITY;
+        }
+      }
+    }
+    // ---- online softmax, the reference raised where a logit lies more than 2^kRescaleSlack above it
+    float mx[NT], over = -INFINITY;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      mx[nt] = max8(s[0][4 * nt], s[0][4 * nt + 1], s[0][4 * nt + 2], s[0][4 * nt + 3], s[1][4 * nt], s[1][4 * nt + 1], s[1][4 * nt + 2], s[1][4 * nt + 3]);
+      over = fmaxf(over, fmaf(mx[nt], sl, nm[nt]));
+    }
+    if (__any(over > kRescaleSlack)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const float nm_new = fminf(nm[nt], -max_over_groups(mx[nt]) * sl);
+        const float alpha = fast_exp2(nm_new - nm[nt]);  // (nm = kNoKey: 0)
+        nm[nt] = nm_new;
+        l[nt] *= alpha;
+#pragma unroll
+        for (int x = 0; x < OT; ++x)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[nt][x][r] *= alpha;
+      }
+    }
+    bf16x8 pf[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float p = fast_exp2(fmaf(s[m][4 * nt + r], sl, nm[nt]));
+          l[nt] += p;
+          pf[nt][4 * m + r] = (__bf16)p;
+        }
+    // ---- O^T += V^T P^T
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const unsigned char* p = area + (4 * G + (c >> 2)) * PITCH + 32 * dt + 8 * (c & 3);
+      const short4v x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)p);
+      const short4v x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)(p + 16 * PITCH));
+      const short8v both = __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7);
+      const bf16x8 v = __builtin_bit_cast(bf16x8, both);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+        set_quarter(o[nt][dt >> 2], dt & 3, __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[nt], quarter(o[nt][dt >> 2], dt & 3), 0, 0, 0));
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int x = 0; x < OT; ++x) asm volatile("" : "+v"(o[nt][x]));
+  }
+
+  // ---- merge the four waves: each scales its part, 16 rows at a time are added through LDS
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const float sum = sum_over_groups(l[nt]);
+    if (G == 0) sref[wave][16 * nt + c] = nm[nt], ssum[wave][16 * nt + c] = sum;
+  }
+  const long long rows = (long long)w.B * w.Hq * w.Lq;
+  const bool parts = a.f.splits > 1;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    __syncthreads();  // (the exchange values are there; the areas are free)
+    const int mine = 16 * nt + c;
+    float ref = sref[0][mine];
+#pragma unroll
+    for (int x = 1; x < 4; ++x) ref = fminf(ref, sref[x][mine]);
+    float total = 0.f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) total += ssum[x][mine] * fast_exp2(ref - sref[x][mine]);  // (no keys: sum 0)
+    const float f = total > 0.f ? fast_exp2(ref - nm[nt]) / total : 0.f;
+    float* const dst = reinterpret_cast<float*>(area) + c * OPITCH + 4 * G;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const f32x4 x = quarter(o[nt][dt >> 2], dt & 3);
+      *reinterpret_cast<float4*>(dst + 16 * dt) = make_float4(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+    }
+    __syncthreads();
+    // thread: row threadIdx / 16 of the 16, channels D / 16 * (threadIdx % 16) ..
+    constexpr int CH = D / 16;
+    const int r = threadIdx.x >> 4, ch = CH * (threadIdx.x & 15), row = row0 + 16 * nt + r;
+    if (row < row1) {
+      const int i = row / w.group, h = hk * w.group + row % w.group;
+      const long long id = ((long long)b * w.Hq + h) * w.Lq + i;
+      const int2 range = srange[16 * nt + r];
+      const bool live = range.y > 0;
+      float best = sref[0][16 * nt + r], sum = 0.f;
+#pragma unroll
+      for (int x = 1; x < 4; ++x) best = fminf(best, sref[x][16 * nt + r]);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) sum += ssum[x][16 * nt + r] * fast_exp2(best - sref[x][16 * nt + r]);
+      const bool some = live && sum > 0.f;
+#pragma unroll
+      for (int e = 0; e < CH; e += 4) {
+        float4 val = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float4 y = *reinterpret_cast<const float4*>(smem + x * AREA + (r * OPITCH + ch + e) * 4);
+          val.x += y.x, val.y += y.y, val.z += y.z, val.w += y.w;
+        }
+        if (!some) val = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (parts) store4<true>(a.f.part_o + (blockIdx.y * rows + id) * D + ch + e, val, 0);
+        else store4<false>(static_cast<unsigned char*>(a.f.out) + b * a.f.so.batch + h * a.f.so.head + i * a.f.so.token + (ch + e) * 2, val, 0);
+      }
+      if ((threadIdx.x & 15) == 0) {
+        const float lse = some ? (__log2f(sum) - best) * kLn2 : -INFINITY;
+        if (parts) a.f.part_lse[blockIdx.y * rows + id] = lse;
+        else if (a.f.lse) a.f.lse[id] = lse;
+      }
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t st) {
+  const WindowShape& w = a.f.w;
+  const int rows = cache_attn_rows(w), tiles = (w.Lq * w.group + rows - 1) / rows;
+  const dim3 grid((unsigned)(tiles * w.B * w.Hkv), a.f.splits);
+  auto go = [&](auto d, auto bits) {
+    constexpr int D = decltype(d)::value, BITS = decltype(bits)::value;
+    if (rows == 16) cache_attn<D, BITS, 1><<<grid, 256, 0, st>>>(a, tiles);
+    else cache_attn<D, BITS, 4><<<grid, 256, 0, st>>>(a, tiles);
+  };
+  using D128 = std::integral_constant<int, 128>;
+  using D64 = std::integral_constant<int, 64>;
+  using B4 = std::integral_constant<int, 4>;
+  using B8 = std::integral_constant<int, 8>;
+  if (a.c.d == 128) a.c.bits == 4 ? go(D128{}, B4{}) : go(D128{}, B8{});
+  else a.c.bits == 4 ? go(D64{}, B4{}) : go(D64{}, B8{});
+  return hipGetLastError();
+}
+
+}  // namespace usv

@@ -71,15 +71,14 @@ __host__ __device__ inline WindowRange window_range(const WindowShape& w, int n,
 }
 __host__ __device__ inline bool window_sees(const WindowRange& r, int sink, int j) { return j < r.hi && (j >= r.lo || j < sink); }
 
-// Keys of the rows [blk * rows, + rows), sinks ahead of the window: entry i of the list is key i where i < head, else i + skip.
+// Keys of the rows [r0, r0 + rows), sinks ahead of the window: entry i of the list is key i where i < head, else i + skip.
 struct WindowKeys {
   int i0, i1;       // rows of the block that hold a token (i0 >= i1: none)
   int head, skip, count;
   int all_hi, all_lo, all_sink;  // every row sees the keys [all_lo, all_hi) and [0, all_sink)
 };
-__host__ __device__ inline WindowKeys window_keys(const WindowShape& w, const WindowSeq& s, int blk, int rows) {
+__host__ __device__ inline WindowKeys window_keys(const WindowShape& w, const WindowSeq& s, long long r0, int rows) {
   WindowKeys k;
-  const long long r0 = (long long)blk * rows;
   long long i0 = -(long long)s.first, i1 = (long long)s.n - s.first;
   if (i0 < r0) i0 = r0;
   if (i1 > r0 + rows) i1 = r0 + rows;

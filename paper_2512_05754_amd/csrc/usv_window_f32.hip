@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256) void window_fwd(WindowArgs a) {
   const WindowSlot at_ = window_slot(a.w, blockIdx.x, blocks);
   const int hk = at_.h / a.w.group;
   const WindowSeq seq = window_seq_of(a.w, at_.b);
-  const WindowKeys keys = window_keys(a.w, seq, at_.blk, kWindowRows);
+  const WindowKeys keys = window_keys(a.w, seq, (long long)at_.blk * kWindowRows, kWindowRows);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, G = lane >> 4;
   const int row = at_.blk * kWindowRows + 16 * wave + c;
   const bool live = row >= keys.i0 && row < keys.i1;
@@ -178,28 +178,50 @@ __global__ __launch_bounds__(256) void window_fwd(WindowArgs a) {
   }
 }
 
-// out = sum of the pieces, each weighed with its share exp(lse_piece - lse).  One wave per 256 / D ... rows: D / 4 lanes a row.
-template <typename T, int D>
+// out = sum of the pieces, each weighed with its share exp(lse_piece - lse).  TPR threads a row: D / 4 of them hold a piece's row, the
+// others take other pieces, so that many are on their way at once.
+template <typename T, int D, int TPR>
 __global__ __launch_bounds__(256) void window_join(WindowArgs a) {
+  constexpr int RPW = 256 / TPR, LPP = D / 4, AT_ONCE = TPR / LPP;  // rows of a workgroup, lanes a piece, pieces at once
+  __shared__ float4 sacc[RPW][AT_ONCE][LPP];
+  __shared__ float sl[RPW][AT_ONCE], smax[RPW][TPR / 64];
   const long long rows = (long long)a.w.B * a.w.Hq * a.w.Lq;
-  const long long id = (long long)blockIdx.x * (1024 / D) + threadIdx.x / (D / 4);
-  if (id >= rows) return;
-  const int ch = 4 * (threadIdx.x % (D / 4));
+  const int r = threadIdx.x / TPR, t = threadIdx.x % TPR, piece = t / LPP, ch = 4 * (t % LPP);
+  const long long want = (long long)blockIdx.x * RPW + r, id = want < rows ? want : rows - 1;
   float m = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_lse[s * rows + id]);
+  for (int s = t; s < a.splits; s += TPR) m = fmaxf(m, a.part_lse[s * rows + id]);
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
+  if constexpr (TPR > 64) {
+    if ((t & 63) == 0) smax[r][t >> 6] = m;
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < TPR / 64; ++x) m = fmaxf(m, smax[r][x]);
+  }
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float l = 0.f;
   if (m != -INFINITY) {
-    for (int s = 0; s < a.splits; ++s) {
-      const float w = fast_exp2((a.part_lse[s * rows + id] - m) * kLog2e);
-      if (w == 0.f) continue;  // (a piece without keys)
+#pragma unroll 4
+    for (int s = piece; s < a.splits; s += AT_ONCE) {
+      const float w = fast_exp2((a.part_lse[s * rows + id] - m) * kLog2e);  // (a piece without keys: 0, and its row holds zeros)
       const float4 x = load4(a.part_o + (s * rows + id) * D + ch);
       l += w;
       acc.x = fmaf(w, x.x, acc.x), acc.y = fmaf(w, x.y, acc.y), acc.z = fmaf(w, x.z, acc.z), acc.w = fmaf(w, x.w, acc.w);
     }
-    const float inv = 1.f / l;
-    acc.x *= inv, acc.y *= inv, acc.z *= inv, acc.w *= inv;
   }
+  sacc[r][piece][t % LPP] = acc;
+  if (ch == 0) sl[r][piece] = l;
+  __syncthreads();
+  if (piece != 0 || want >= rows) return;
+  acc = make_float4(0.f, 0.f, 0.f, 0.f), l = 0.f;
+#pragma unroll
+  for (int x = 0; x < AT_ONCE; ++x) {
+    const float4 y = sacc[r][x][t];
+    l += sl[r][x];
+    acc.x += y.x, acc.y += y.y, acc.z += y.z, acc.w += y.w;
+  }
+  const float inv = m != -INFINITY ? 1.f / l : 0.f;
+  acc.x *= inv, acc.y *= inv, acc.z *= inv, acc.w *= inv;
   const int row = (int)(id % a.w.Lq), bh = (int)(id / a.w.Lq);
   put4<T>(row_of<T>(a.out, a.so, bh / a.w.Hq, bh % a.w.Hq, row) + ch, acc);
   if (a.lse && ch == 0) a.lse[id] = m == -INFINITY ? -INFINITY : m + __log2f(l) * kLn2;
@@ -213,7 +235,7 @@ __global__ __launch_bounds__(256) void window_grad_q(WindowGradArgs g) {
   const WindowSlot at_ = window_slot(a.w, blockIdx.x, blocks);
   const int hk = at_.h / a.w.group;
   const WindowSeq seq = window_seq_of(a.w, at_.b);
-  const WindowKeys keys = window_keys(a.w, seq, at_.blk, kWindowRows);
+  const WindowKeys keys = window_keys(a.w, seq, (long long)at_.blk * kWindowRows, kWindowRows);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, G = lane >> 4;
   const int row = at_.blk * kWindowRows + 16 * wave + c;
   const bool live = row >= keys.i0 && row < keys.i1;
@@ -397,8 +419,11 @@ hipError_t launch_window_f32(const WindowArgs& a, bool bf16, int d, hipStream_t 
 }
 
 hipError_t launch_window_join(const WindowArgs& a, bool bf16, int d, hipStream_t st) {
-  const long long rows = (long long)a.w.B * a.w.Hq * a.w.Lq, per = 1024 / d;
-  return by_type(bf16, d, [&](auto t, auto dc) { window_join<decltype(t), decltype(dc)::value><<<(unsigned)((rows + per - 1) / per), 256, 0, st>>>(a); });
+  const long long rows = (long long)a.w.B * a.w.Hq * a.w.Lq;
+  return by_type(bf16, d, [&](auto t, auto dc) {
+    if (a.splits > 8) window_join<decltype(t), decltype(dc)::value, 256><<<(unsigned)rows, 256, 0, st>>>(a);
+    else window_join<decltype(t), decltype(dc)::value, 64><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a);
+  });
 }
 
 hipError_t launch_window_grad_f32(const WindowGradArgs& g, bool bf16, int d, hipStream_t st) {
