@@ -828,7 +828,7 @@ usv_status usv_window_attn(const void* q, const void* k, const void* v, const us
   window_set_parts(&a, d, splits, ws);
   if (w->q_len == 0) return hip_result(hipSuccess, "");
   hipStream_t st = static_cast<hipStream_t>(stream);
-  hipError_t e = usv::launch_window_f32(a, bf16, d, st);
+  hipError_t e = bf16 ? usv::launch_window_bf16(a, d, st) : usv::launch_window_f32(a, d, st);
   if (e == hipSuccess && splits > 1) e = usv::launch_window_join(a, bf16, d, st);
   return hip_result(e, "usv_window_attn");
 }

@@ -69,7 +69,8 @@ __host__ __device__ inline WindowRange window_range(const WindowShape& w, int n,
   r.lo = w.left < 0 || begin < 0 ? 0 : (int)begin;
   return r;
 }
-__host__ __device__ inline bool window_sees(const WindowRange& r, int sink, int j) { return j < r.hi && (j >= r.lo || j < sink); }
+// (bits, not branches)
+__host__ __device__ inline bool window_sees(const WindowRange& r, int sink, int j) { return (j < r.hi) & ((j >= r.lo) | (j < sink)); }
 
 // Keys of the rows [r0, r0 + rows), sinks ahead of the window: entry i of the list is key i where i < head, else i + skip.
 struct WindowKeys {
@@ -92,6 +93,12 @@ __host__ __device__ inline WindowKeys window_keys(const WindowShape& w, const Wi
   k.count = z.hi - k.skip;
   k.all_hi = a.hi, k.all_lo = z.lo, k.all_sink = w.sink < a.hi ? w.sink : a.hi;
   return k;
+}
+__device__ __forceinline__ void window_uniform(WindowKeys* k) {  // (the same in every lane: kept in scalar registers)
+  k->i0 = __builtin_amdgcn_readfirstlane(k->i0), k->i1 = __builtin_amdgcn_readfirstlane(k->i1);
+  k->head = __builtin_amdgcn_readfirstlane(k->head), k->skip = __builtin_amdgcn_readfirstlane(k->skip);
+  k->count = __builtin_amdgcn_readfirstlane(k->count), k->all_hi = __builtin_amdgcn_readfirstlane(k->all_hi);
+  k->all_lo = __builtin_amdgcn_readfirstlane(k->all_lo), k->all_sink = __builtin_amdgcn_readfirstlane(k->all_sink);
 }
 // Whether every row sees all the entries [t, t + tile).
 __host__ __device__ inline bool window_tile_open(const WindowKeys& k, int t, int tile) {
@@ -122,21 +129,22 @@ __host__ __device__ inline WindowRows window_rows(const WindowShape& w, const Wi
   return {(int)i0, (int)i1};
 }
 
-// Launch slot -> (block of rows, head).  Later blocks of rows see more keys (up to the window), so the launch begins with them; the
-// heads are spread over the XCDs, the query heads of one key head on the same one as far as the numbers allow.
+// Launch slot -> (block of rows, head).  Slots go round the 8 XCDs.  An XCD takes the key heads one after the other, all rows of all query heads
+// that share one (its workgroups of a time then sweep the same keys, which its L2 serves); what is left of the key heads, fewer than 8,
+// is spread over the XCDs.  Within a key head the launch begins with the last rows, which see the most keys.
 struct WindowSlot {
   int blk, b, h;
 };
 __device__ __forceinline__ WindowSlot window_slot(const WindowShape& w, int slot, int blocks) {
-  const int heads = w.B * w.Hq;
-  const int blk = blocks - 1 - slot / heads;
-  const int r = slot % heads;
-  int bh = r;
-  if (heads % kNumXcd == 0) {  // slots go round the XCDs: XCD x gets heads / 8 neighbouring heads
-    const int per = heads / kNumXcd;
-    bh = (r % kNumXcd) * per + r / kNumXcd;
+  const int heads = w.B * w.Hkv, items = blocks * w.group, whole = heads / kNumXcd;
+  int y = slot / kNumXcd, unit, item;
+  if (y < whole * items) {
+    unit = y / items * kNumXcd + slot % kNumXcd, item = y % items;
+  } else {
+    const int z = slot - whole * items * kNumXcd, rest = heads % kNumXcd;
+    unit = whole * kNumXcd + z % rest, item = z / rest;
   }
-  return {blk, bh / w.Hq, bh % w.Hq};
+  return {blocks - 1 - item / w.group, unit / w.Hkv, unit % w.Hkv * w.group + item % w.group};
 }
 
 // Gradient of the keys: launch slot -> (key block, piece of its list of rows, head).  Blocks that every row sees come first, in pieces of
@@ -171,7 +179,8 @@ __device__ __forceinline__ WindowPiece window_piece(const WindowGradArgs& g, int
 
 constexpr int kWindowRows = 64;  // query rows of a workgroup
 
-hipError_t launch_window_f32(const WindowArgs& a, bool bf16, int d, hipStream_t st);
+hipError_t launch_window_f32(const WindowArgs& a, int d, hipStream_t st);
+hipError_t launch_window_bf16(const WindowArgs& a, int d, hipStream_t st);
 hipError_t launch_window_join(const WindowArgs& a, bool bf16, int d, hipStream_t st);
 hipError_t launch_window_grad_f32(const WindowGradArgs& a, bool bf16, int d, hipStream_t st);
 hipError_t launch_window_grad_join(const WindowGradArgs& a, bool bf16, int d, hipStream_t st);

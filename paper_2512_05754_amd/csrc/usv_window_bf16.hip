@@ -1,0 +1,454 @@
+// Windowed attention with sinks, bf16, forward.
+//
+// One workgroup = 2 wavefronts = 64 query rows of one head.  Wave w owns all 64 rows and every other stretch of 32 entries of the block's
+// key list, with an online softmax of its own; the two results are merged once, at the end.  A wave fetches, waits for and
+// reads its own K and V only, so the main loop has no barrier, and a fragment read from LDS feeds four MFMAs.
+//
+// Matrix cores (v_mfma_f32_16x16x32_bf16; lane = (c, G), c = lane % 16, G = lane / 16):
+//   S^T (16 keys x 16 queries) = K Q^T, D / 32 steps over the channels;  O^T (16 channels x 16 queries) += V^T P^T, one step over the 32 keys
+// on the transposes: a lane column is a query, whose statistics stay in four lanes, and the eight S^T values that a lane holds of a
+// query are, as they stand, the eight contraction slots of its P^T operand.  V^T comes from row-major V with ds_read_b64_tr_b16.
+//
+// LDS: an item is 32 keys x 64 channels of K or V (a 128-byte line of every row, 4 KiB), four global_load_lds_dwordx4 of 8 rows each.
+// A wave holds one step's items (D / 64 of K, D / 64 of V); as soon as the last fragment of an item is in registers, its place takes the same item
+// of the next step.  The 16-byte chunks of a line are XOR-permuted on the global side so that K reads and transposing V reads are free of
+// bank conflicts.
+//
+// Addresses: a step whose 32 entries are neighbouring keys (all but the one that joins the sinks to the window and the last one) is
+// fetched from scalar row addresses that move on by a constant, with fixed lane offsets: no vector instruction for any stride.  The
+// other steps compute a full address per lane.
+//
+// The weights are rounded to bf16 for the second product; their sum is taken unrounded, in fp32.
+#include "usv_attn_bf16.h"
+#include "usv_window.h"
+
+namespace usv {
+namespace {
+
+constexpr int NW = 2;
+constexpr int kItem = 4096;
+constexpr int kStep = 32;                // entries of a wave's step
+constexpr float kNoKey = 3.4028234e38f;  // reference of a row that has seen no key yet
+
+// One item, global -> LDS: instruction r takes rows 8 r .. 8 r + 7 and lands at lds + 1024 r + 16 * lane.  Its offset field is added to the
+// global and the LDS address, so base r is short of it; LINE 1 is 128 bytes further in global memory, and lds is short of those.
+// M0 carries the LDS address; nothing else in this kernel uses it.
+template <int LINE>
+__device__ __forceinline__ void dma_rows(unsigned lds, const unsigned long long (&base)[4], unsigned even, unsigned odd) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "global_load_lds_dwordx4 %1, %3 offset:%7\n\t"
+      "global_load_lds_dwordx4 %2, %4 offset:%8\n\t"
+      "global_load_lds_dwordx4 %1, %5 offset:%9\n\t"
+      "global_load_lds_dwordx4 %2, %6 offset:%10"
+      :
+      : "s"(lds - 128 * LINE), "v"(even), "v"(odd), "s"(base[0]), "s"(base[1]), "s"(base[2]), "s"(base[3]), "n"(128 * LINE), "n"(1024 + 128 * LINE), "n"(2048 + 128 * LINE),
+        "n"(3072 + 128 * LINE)
+      : "memory");
+}
+__device__ __forceinline__ void dma_lane(unsigned lds, unsigned long long addr) {  // 64 lanes, an address each
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(addr) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("s_waitcnt lgkmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ unsigned long long uniform(unsigned long long x) {
+  return ((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)x);
+}
+
+// The arguments, read again where they are asked for: kept over the loop they are scalar registers that it has not got.
+__device__ __forceinline__ const WindowArgs& again(const WindowArgs& a) {
+  unsigned long long p = reinterpret_cast<unsigned long long>(__builtin_amdgcn_kernarg_segment_ptr());
+  asm volatile("" : "+s"(p));
+  return *reinterpret_cast<const WindowArgs*>(p);
+}
+
+template <int D, int WPS, int QL_>
+__global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
+  constexpr int KS = D / 32, DT = D / 16, OT = (DT + 3) / 4;
+  constexpr int LINES = D / 64, IPS = 2 * LINES;
+  constexpr int KF = 3, VF = 2;  // fragments of K, V in flight
+  constexpr int QL = QL_;        // Q fragments of the last channel step that are read back from LDS: there are no registers for them
+  constexpr int XROWS = DT * 8 + 4;
+  constexpr int OSTRIDE = D + 4;
+  constexpr int kWaveBytes = IPS * kItem > XROWS * 256 ? IPS * kItem : XROWS * 256;  // items, later the exchange area
+  static_assert(XROWS * 64 >= 32 * OSTRIDE, "the staging rows of 32 queries overlay an exchange area");
+  static_assert(kWaveBytes % 1024 == 0, "fragment addresses are formed with XOR below bit 10");
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * kWaveBytes];
+  __shared__ int2 srange[kWindowRows];
+  __shared__ __attribute__((aligned(16))) unsigned char q_tail[QL > 0 ? QL * 1024 : 16];
+
+  const WindowShape& w = a.w;
+  const WindowSlot slot = window_slot(w, blockIdx.x, (w.Lq + kWindowRows - 1) / kWindowRows);
+  const WindowSeq seq = window_seq_of(w, slot.b);
+  const int row0 = slot.blk * kWindowRows;
+  WindowKeys keys = window_keys(w, seq, row0, kWindowRows);
+  window_uniform(&keys);
+  const int lane = threadIdx.x & 63, c16 = lane & 15, G = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  // entries of this workgroup: tiles of 64; this wave's steps are at first + 64 n
+  const int tiles = (keys.count + 63) / 64;
+  const int t0 = (int)((long long)tiles * blockIdx.y / a.splits), t1 = (int)((long long)tiles * (blockIdx.y + 1) / a.splits);
+  const int first = t0 * 64 + wave * kStep, end = min(t1 * 64, keys.count);
+  const int n_steps = __builtin_amdgcn_readfirstlane(first < end ? (end - first + 63) / 64 : 0);
+
+  if (threadIdx.x < kWindowRows) {
+    const int row = row0 + threadIdx.x;
+    const WindowRange r = row >= keys.i0 && row < keys.i1 ? window_range(w, seq.n, seq.first + row) : WindowRange{0, 0};
+    srange[threadIdx.x] = make_int2(r.lo, r.hi);
+  }
+
+  const int hk = slot.h / w.group;
+  const unsigned wave_lds = lds_address(smem) + wave * kWaveBytes;
+  // DMA lane -> row lane / 8 of an instruction's 8 rows, 16-byte chunk lane % 8 of the line; K chunks are stored at chunk ^ (row / 2 % 8), V
+  // chunks at chunk ^ 2 (row / 2 % 4)
+  const unsigned kchunk = ((lane & 7) ^ (lane >> 4)) << 4, vchunk = ((lane & 7) ^ (((lane >> 4) & 3) << 1)) << 4;
+  const unsigned k_even = (lane >> 3) * (unsigned)a.sk.token + kchunk, k_odd = (lane >> 3) * (unsigned)a.sk.token + (kchunk ^ 64);
+  const unsigned v_all = (lane >> 3) * (unsigned)a.sv.token + vchunk;
+  // rows 8 r of the step to be requested next, short of what the instruction's offset field adds
+  unsigned long long kb[4], vb[4];
+  auto point_at = [&](int entry) {
+    const long long key = window_key(keys, entry);
+    const WindowArgs& b = again(a);
+    const unsigned long long kb0 = reinterpret_cast<unsigned long long>(b.k) + slot.b * b.sk.batch + hk * b.sk.head;
+    const unsigned long long vb0 = reinterpret_cast<unsigned long long>(b.v) + slot.b * b.sv.batch + hk * b.sv.head;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      kb[r] = uniform(kb0 + (key + 8 * r) * b.sk.token - 1024 * r);
+      vb[r] = uniform(vb0 + (key + 8 * r) * b.sv.token - 1024 * r);
+    }
+  };
+  const unsigned long long kmove = uniform(64ull * a.sk.token), vmove = uniform(64ull * a.sv.token);
+  auto plain_step = [&](int e) { return e + kStep <= keys.count && (e >= keys.head || e + kStep <= keys.head); };
+  // item x of the step that kb, vb point at
+  auto dma = [&](auto x_c) {
+    constexpr int x = decltype(x_c)::value, LINE = x % LINES;
+    const unsigned lds = wave_lds + x * kItem;
+    if constexpr (x < LINES) dma_rows<LINE>(lds, kb, k_even, k_odd);
+    else dma_rows<LINE>(lds, vb, v_all, v_all);
+  };
+  // all items of any step; entries past the list's end take its last key (the mask takes them out)
+  auto dma_step = [&](int e) {
+    int ln = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+    asm volatile("" : "+v"(ln));  // formed here, on the rare path
+    const WindowArgs& b = again(a);
+    const unsigned long long kb0 = reinterpret_cast<unsigned long long>(b.k) + slot.b * b.sk.batch + hk * b.sk.head;
+    const unsigned long long vb0 = reinterpret_cast<unsigned long long>(b.v) + slot.b * b.sv.batch + hk * b.sv.head;
+#pragma unroll 1
+    for (int r = 0; r < 4; ++r) {
+      const long long key = window_key(keys, min(e + 8 * r + (ln >> 3), keys.count - 1));
+      const unsigned kc = ((ln & 7) ^ (((4 * r) & 7) ^ (ln >> 4))) << 4, vc = ((ln & 7) ^ (((ln >> 4) & 3) << 1)) << 4;
+#pragma unroll
+      for (int line = 0; line < LINES; ++line) {
+        dma_lane(wave_lds + line * kItem + 1024 * r, kb0 + key * b.sk.token + line * 128 + kc);
+        dma_lane(wave_lds + (LINES + line) * kItem + 1024 * r, vb0 + key * b.sv.token + line * 128 + vc);
+      }
+    }
+  };
+  using I0 = std::integral_constant<int, 0>;
+  using I1 = std::integral_constant<int, 1>;
+  using I2 = std::integral_constant<int, 2>;
+  using I3 = std::integral_constant<int, 3>;
+  if (n_steps > 0) {
+    point_at(first);
+    if (plain_step(first)) {
+      dma(I0{});
+      dma(I1{});
+      if constexpr (IPS == 4) {
+        dma(I2{});
+        dma(I3{});
+      }
+    } else {
+      dma_step(first);
+    }
+  }
+
+  // Q fragments: for query tile nt the lane holds row 16 nt + c16, channels 32 t + 8 G .. + 8 for every step t
+  bf16x8 qf[4][KS];
+  if (n_steps > 0) {
+#pragma unroll
+    for (int nt = 0; nt < 4; ++nt) {
+      const int row = min(max(row0 + 16 * nt + c16, keys.i0), keys.i1 - 1);
+      const uint16_t* qp = reinterpret_cast<const uint16_t*>(static_cast<const unsigned char*>(a.q) + slot.b * a.sq.batch + slot.h * a.sq.head + row * a.sq.token) + G * 8;
+#pragma unroll
+      for (int t = 0; t < KS; ++t) qf[nt][t] = *reinterpret_cast<const bf16x8*>(qp + t * 32);
+    }
+  }
+  if constexpr (QL > 0) {  // (both waves write the same values, and a wave reads back what it wrote itself)
+#pragma unroll
+    for (int e = 0; e < QL; ++e) *reinterpret_cast<bf16x8*>(q_tail + e * 1024 + lane * 16) = qf[4 - QL + e][KS - 1];
+  }
+  f32x16 o[4][OT];
+#pragma unroll
+  for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+    for (int x = 0; x < OT; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[nt][x][r] = 0.f;
+  // Per query tile: nm = -(reference maximum) in the log2 domain, identical in the four lanes of its query; l = this lane's share of the sum
+  float nm[4], l[4];
+#pragma unroll
+  for (int nt = 0; nt < 4; ++nt) nm[nt] = kNoKey, l[nt] = 0.f;
+  const float sl = a.scale * kLog2e;
+
+  // Lane bases of the fragment reads.  K fragment (mt, t): row 16 mt + c16, chunks 4 t + G.  V^T fragment of channel tile dt: slots 0..3 are rows
+  // 4 G + (0..3), slots 4..7 rows 16 + 4 G + (0..3), the order in which the S^T accumulators hold the keys.
+  unsigned kl = wave * kWaveBytes + (c16 >> 3) * 1024 + (c16 & 7) * 128 + ((G ^ (c16 >> 1)) << 4);
+  unsigned vl = wave * kWaveBytes + (G >> 1) * 1024 + (4 * (G & 1) + (c16 >> 2)) * 128 +
+                ((((c16 >> 1) & 1) ^ (((2 * (G & 1) + (c16 >> 3)) & 3) << 1)) << 4) + (c16 & 1) * 8;
+
+  __syncthreads();  // srange
+  wait_vm<0>();     // the first step and Q have landed
+#pragma unroll
+  for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+    for (int t = 0; t < KS; ++t)
+      if (t < KS - 1 || nt < 4 - QL) asm volatile("" : "+v"(qf[nt][t]));  // (else their loads sink into the loop, with waits for all memory)
+
+  // One step.  The next one is fetched item by item while this one is worked on, if it is of the plain kind; else all of it behind this one.
+  auto step = [&](int n) {
+    const int e0 = first + 64 * n, e1 = e0 + 64;
+    const bool more = n + 1 < n_steps, ahead = more && plain_step(e1);
+    if (!ahead) {
+      wait_vm<0>();
+    } else if (e0 >= keys.head || e1 < keys.head) {  // on in the same stretch
+#pragma unroll
+      for (int r = 0; r < 4; ++r) kb[r] += kmove, vb[r] += vmove;
+    } else {
+      point_at(e1);
+    }
+    // Item x of this step is in LDS.  Younger requests: the items behind it and those of the next step asked for by then (none: nothing is
+    // under way any more).
+    auto await = [&](auto x_c) {
+      constexpr int x = decltype(x_c)::value;
+      wait_vm<(LINES == 2 && (x & 1) ? IPS - 2 : IPS - 1) * 4>();
+    };
+    auto refill = [&](auto x_c) {
+      if (ahead) dma(x_c);
+    };
+
+    // ---- S^T = K Q^T: s[mt], quarter nt = tile (mt, nt) ----
+    f32x16 s[2];
+    asm volatile("" : "+v"(kl), "+v"(vl));  // keeps the XORs in the loop
+    bf16x8 kf[KF], ql[QL > 0 ? QL : 1];
+    auto read_k = [&](int f) {  // fragment f = 2 t + mt
+      kf[f % KF] = *reinterpret_cast<const bf16x8*>(smem + ((kl + (f >> 2) * kItem) ^ (((f >> 1) & 1) << 6)) + (f & 1) * 2048);
+    };
+    await(I0{});
+#pragma unroll
+    for (int f = 0; f < KF - 1; ++f) read_k(f);
+#pragma unroll
+    for (int f = 0; f < 2 * KS; ++f) {
+      if (LINES == 2 && f + KF - 1 == 4) await(I1{});
+      if (f + KF - 1 < 2 * KS) read_k(f + KF - 1);
+      if (f == 3) {
+        wait_lds<(LINES == 2 ? KF - 1 : 0)>();
+        refill(I0{});
+      }
+      if (LINES == 2 && f == 2 * KS - 2) {
+        wait_lds<0>();
+        refill(I1{});
+      }
+      if (QL > 0 && f == 2 * KS - 2) {  // (for the last two fragments)
+        int ln = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+        asm volatile("" : "+v"(ln));
+#pragma unroll
+        for (int e = 0; e < QL; ++e) ql[e] = *reinterpret_cast<const bf16x8*>(q_tail + ln * 16 + e * 1024);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int nt = 0; nt < 4; ++nt) {
+        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+        set_quarter(s[f & 1], nt, __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[f % KF], QL > 0 && f >= 2 * KS - 2 && nt >= 4 - QL ? ql[nt >= 4 - QL ? nt - (4 - QL) : 0] : qf[nt][f >> 1], f < 2 ? zero : quarter(s[f & 1], nt), 0, 0, 0));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("" : "+v"(s[f & 1]));
+    }
+
+    // s[mt][4 nt + r] is entry e0 + 16 mt + 4 G + r, query 16 nt + c16
+    if (!window_tile_open(keys, e0, kStep)) {
+      int ln = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+      asm volatile("" : "+v"(ln));
+#pragma unroll
+      for (int nt = 0; nt < 4; ++nt) {
+        const int2 rr = srange[16 * nt + (ln & 15)];
+        const WindowRange range = {rr.x, rr.y};
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int e = e0 + 16 * mt + 4 * (ln >> 4) + r;
+            s[mt][4 * nt + r] = (e < keys.count) & window_sees(range, w.sink, window_key(keys, e)) ? s[mt][4 * nt + r] : -INFINITY;
+          }
+      }
+    }
+
+    // ---- online softmax (log2 domain, lazily raised reference) ----
+    float mx[4];
+#pragma unroll
+    for (int nt = 0; nt < 4; ++nt)
+      mx[nt] = max8(s[0][4 * nt], s[0][4 * nt + 1], s[0][4 * nt + 2], s[0][4 * nt + 3], s[1][4 * nt], s[1][4 * nt + 1], s[1][4 * nt + 2], s[1][4 * nt + 3]);
+    float over = fmaf(mx[0], sl, nm[0]);
+#pragma unroll
+    for (int nt = 1; nt < 4; ++nt) over = fmaxf(over, fmaf(mx[nt], sl, nm[nt]));
+    if (__any(over > kRescaleSlack)) {  // wave-uniform; always taken on the first live step
+#pragma unroll
+      for (int nt = 0; nt < 4; ++nt) {
+        const float nm_new = fminf(nm[nt], -max_over_groups(mx[nt]) * sl);
+        const float alpha = fast_exp2(nm_new - nm[nt]);  // (nm = kNoKey: 0)
+        nm[nt] = nm_new;
+        l[nt] *= alpha;
+#pragma unroll
+        for (int x = 0; x < OT; ++x)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[nt][x][r] *= alpha;
+      }
+    }
+    bf16x8 pf[4];
+#pragma unroll
+    for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float p = fast_exp2(fmaf(s[mt][4 * nt + r], sl, nm[nt]));
+          l[nt] += p;
+          pf[nt][4 * mt + r] = (__bf16)p;
+        }
+
+    // ---- O^T += V^T P^T ----
+    bf16x8 vf[VF];
+    auto read_v = [&](int dt) {
+      const unsigned char* p = smem + ((vl + (LINES + (dt >> 2)) * kItem) ^ ((dt & 3) << 5));
+      const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)p);
+      const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)(p + 2048));
+      vf[dt % VF] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    await(std::integral_constant<int, LINES>{});
+#pragma unroll
+    for (int dt = 0; dt < VF - 1; ++dt) read_v(dt);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      if (LINES == 2 && dt + VF - 1 == 4) await(I3{});
+      if (dt + VF - 1 < DT) read_v(dt + VF - 1);
+      if (dt == 3) {
+        wait_lds<(LINES == 2 ? 2 * (VF - 1) : 0)>();
+        refill(std::integral_constant<int, LINES>{});
+      }
+      if (LINES == 2 && dt == DT - 1) {
+        wait_lds<0>();
+        refill(I3{});
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int nt = 0; nt < 4; ++nt)
+        set_quarter(o[nt][dt >> 2], dt & 3, __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[dt % VF], pf[nt], quarter(o[nt][dt >> 2], dt & 3), 0, 0, 0));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+      for (int x = 0; x < OT; ++x) asm volatile("" : "+v"(o[nt][x]));
+    if (more && !ahead) {
+      wait_lds<0>();
+      dma_step(e1);
+      point_at(e1);
+    }
+  };
+  for (int n = 0; n < n_steps; ++n) step(n);
+  const WindowArgs& z = again(a);
+
+  // ---- merge the two waves, stage the rows in LDS, store ----
+  // Wave w finishes query tiles 2 w and 2 w + 1: it gives the other two away through its own area (dead by now), adds what the other wave
+  // gave, and stages its rows where it has just read.
+  float l_row[4];
+#pragma unroll
+  for (int nt = 0; nt < 4; ++nt) l_row[nt] = sum_over_groups(l[nt]);
+  auto give = [&](auto first_c) {
+    constexpr int F = decltype(first_c)::value;
+    float* dst = reinterpret_cast<float*>(smem + wave * kWaveBytes) + lane;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) dst[((e * DT + dt) * 4 + r) * 64] = o[F + e][dt >> 2][4 * (dt & 3) + r];
+      dst[(DT * 8 + e) * 64] = nm[F + e];
+      dst[(DT * 8 + 2 + e) * 64] = l_row[F + e];
+    }
+  };
+  const long long rows = (long long)z.w.B * z.w.Hq * z.w.Lq, id0 = ((long long)slot.b * z.w.Hq + slot.h) * z.w.Lq;
+  const bool parts = z.splits > 1;
+  auto take = [&](auto first_c) {
+    constexpr int F = decltype(first_c)::value;
+    float* area = reinterpret_cast<float*>(smem + (wave ^ 1) * kWaveBytes);
+    const float* src = area + lane;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float n1 = src[(DT * 8 + e) * 64], l1 = src[(DT * 8 + 2 + e) * 64];
+      const float ref = fminf(nm[F + e], n1);
+      const float a0 = fast_exp2(ref - nm[F + e]), a1 = fast_exp2(ref - n1);  // (a side without keys: l = 0, O = 0)
+      const float lt = l_row[F + e] * a0 + l1 * a1;
+      const int row = row0 + 16 * (F + e) + c16;
+      const bool live = row >= keys.i0 && row < keys.i1 && lt > 0.f;
+      const float inv = live ? 1.f / lt : 0.f;
+      const float w0 = live ? a0 * inv : 0.f, w1 = live ? a1 * inv : 0.f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float val = o[F + e][dt >> 2][4 * (dt & 3) + r] * w0 + src[((e * DT + dt) * 4 + r) * 64] * w1;
+          o[F + e][dt >> 2][4 * (dt & 3) + r] = live ? val : 0.f;
+        }
+      if (G == 0 && row < z.w.Lq) {
+        const float val = live ? (__log2f(lt) - ref) * kLn2 : -INFINITY;
+        if (parts) z.part_lse[blockIdx.y * rows + id0 + row] = val;
+        else if (z.lse) z.lse[id0 + row] = val;
+      }
+    }
+    wait_lds<0>();  // every exchange value of this wave is in registers before its area is overwritten
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      float* stage = area + (16 * e + c16) * OSTRIDE;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const f32x16& t = o[F + e][dt >> 2];
+        const int x = 4 * (dt & 3);
+        *reinterpret_cast<float4*>(stage + 16 * dt + 4 * G) = make_float4(t[x], t[x + 1], t[x + 2], t[x + 3]);
+      }
+    }
+  };
+  __syncthreads();  // (the other wave's last reads of its area are its own; the areas are given away only behind both loops)
+  if (wave == 0) give(I2{});
+  else give(I0{});
+  __syncthreads();
+  if (wave == 0) take(I0{});
+  else take(I2{});
+  const float* other = reinterpret_cast<const float*>(smem + (wave ^ 1) * kWaveBytes);
+  unsigned char* const dst = static_cast<unsigned char*>(z.out) + slot.b * z.so.batch + slot.h * z.so.head;
+#pragma unroll
+  for (int it = 0; it < 32 * D / 8 / 64; ++it) {
+    const int id = it * 64 + lane, rr = id / (D / 8), ch = (id % (D / 8)) * 8, row = row0 + 32 * wave + rr;
+    if (row >= z.w.Lq) continue;
+    const float4 val[2] = {*reinterpret_cast<const float4*>(other + rr * OSTRIDE + ch), *reinterpret_cast<const float4*>(other + rr * OSTRIDE + ch + 4)};
+    if (parts) store8<true>(z.part_o + (blockIdx.y * rows + id0 + row) * D + ch, val, 0);
+    else store8<false>(dst + row * z.so.token + ch * 2, val, 0);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_window_bf16(const WindowArgs& a, int d, hipStream_t st) {
+  const dim3 grid((unsigned)((a.w.Lq + kWindowRows - 1) / kWindowRows * a.w.B * a.w.Hq), a.splits);
+  if (d == 128) window_fwd_bf16<128, 2, 4><<<grid, 64 * NW, 0, st>>>(a);
+  else window_fwd_bf16<64, 3, 2><<<grid, 64 * NW, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace usv

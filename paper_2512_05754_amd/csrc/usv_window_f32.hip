@@ -413,9 +413,11 @@ hipError_t by_type(bool bf16, int d, F f) {
 
 }  // namespace
 
-hipError_t launch_window_f32(const WindowArgs& a, bool bf16, int d, hipStream_t st) {
+hipError_t launch_window_f32(const WindowArgs& a, int d, hipStream_t st) {
   const dim3 grid((unsigned)((a.w.Lq + kWindowRows - 1) / kWindowRows * a.w.B * a.w.Hq), a.splits);
-  return by_type(bf16, d, [&](auto t, auto dc) { window_fwd<decltype(t), decltype(dc)::value><<<grid, 256, 0, st>>>(a); });
+  if (d == 128) window_fwd<float, 128><<<grid, 256, 0, st>>>(a);
+  else window_fwd<float, 64><<<grid, 256, 0, st>>>(a);
+  return hipGetLastError();
 }
 
 hipError_t launch_window_join(const WindowArgs& a, bool bf16, int d, hipStream_t st) {
