@@ -13,7 +13,7 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libusv.so")
 SOURCES = ("usv_api.hip", "usv_scores.hip", "usv_topk.hip", "usv_attn_f32.hip", "usv_attn_bf16.hip",
            "usv_attn_wide.hip", "usv_reorder.hip", "usv_coarse.hip", "usv_entropy.hip",
-           "usv_merge.hip", "usv_window_f32.hip", "usv_window_bf16.hip", "usv_cache.hip", "usv_cache_attn.hip")
+           "usv_merge.hip", "usv_window_f32.hip", "usv_window_bf16.hip", "usv_window_grad.hip", "usv_cache.hip", "usv_cache_attn.hip")
 
 
 def hipcc() -> str:

@@ -219,14 +219,15 @@ void window_grad_plan(usv::WindowGradArgs* g, int block, int rows_per_tile, int 
   g->sink_parts = parts(sink_list);
   g->parts = parts(longest);
 }
-size_t window_delta_bytes(const usv::WindowShape& s) { return ((size_t)s.B * s.Hq * s.Lq * sizeof(float) + 255) / 256 * 256; }
+size_t window_delta_bytes(const usv::WindowShape& s, bool bf16) { return ((size_t)s.B * s.Hq * s.Lq * (bf16 ? 16 : 4) + 255) / 256 * 256; }
 size_t window_partial_bytes(const usv::WindowGradArgs& g, int d) {
   const size_t heads = (size_t)g.f.w.B * g.f.w.Hkv;
   const size_t slots = heads * ((g.sink_parts > 1 ? (size_t)g.sink_blocks * g.sink_parts : 0) + (g.parts > 1 ? (size_t)(g.blocks - g.sink_blocks) * g.parts : 0));
   return slots * 2 * g.block * d * sizeof(float);
 }
-void window_grad_plan_for(usv::WindowGradArgs* g, const usv_window* w) {
-  window_grad_plan(g, 64, 32, 1024);
+void window_grad_plan_for(usv::WindowGradArgs* g, const usv_window* w) {  // (workgroups: what the chip runs together)
+  if (w->dtype == USV_BF16) window_grad_plan(g, 128, 64, w->head_dim == 128 ? 512 : 768);
+  else window_grad_plan(g, 64, 32, w->head_dim == 128 ? 512 : 768);
 }
 
 usv_status check_cache(const usv_cache* c, usv::CacheShape* s) {
@@ -837,7 +838,7 @@ size_t usv_window_backward_workspace_bytes(const usv_window* w) {
   usv::WindowGradArgs g = {};
   if (check_window(w, &g.f.w) != USV_OK) return 0;
   window_grad_plan_for(&g, w);
-  const size_t n = window_delta_bytes(g.f.w) + window_partial_bytes(g, w->head_dim);
+  const size_t n = window_delta_bytes(g.f.w, w->dtype == USV_BF16) + window_partial_bytes(g, w->head_dim);
   return n ? n : 16;
 }
 
@@ -875,16 +876,16 @@ usv_status usv_window_attn_backward(const void* q, const void* k, const void* v,
   if (!(scale <= 0.f) && !std::isfinite(scale)) return fail(USV_ERR_INVALID_ARG, "scale must be finite");
   window_grad_plan_for(&g, w);
   USV_TRY(check_ptr(ws, "ws"));
-  const size_t need = window_delta_bytes(a.w) + window_partial_bytes(g, d);
+  const size_t need = window_delta_bytes(a.w, bf16) + window_partial_bytes(g, d);
   if (ws_bytes < need) return fail(USV_ERR_WORKSPACE, "ws holds %zu bytes, %zu are needed", ws_bytes, need);
   a.q = q, a.k = k, a.v = v, a.out = const_cast<void*>(out), a.lse = const_cast<float*>(lse);
   a.scale = scale > 0.f ? scale : 1.f / std::sqrt((float)d);
   a.splits = 1;
   g.dout = dout, g.dq = dq, g.dk = dk, g.dv = dv;
   g.delta = static_cast<float*>(ws);
-  g.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + window_delta_bytes(a.w));
+  g.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + window_delta_bytes(a.w, bf16));
   hipStream_t st = static_cast<hipStream_t>(stream);
-  hipError_t e = usv::launch_window_grad_f32(g, bf16, d, st);
+  hipError_t e = bf16 ? usv::launch_window_grad_bf16(g, d, st) : usv::launch_window_grad_f32(g, d, st);
   if (e == hipSuccess && window_partial_bytes(g, d)) e = usv::launch_window_grad_join(g, bf16, d, st);
   return hip_result(e, "usv_window_attn_backward");
 }

@@ -40,7 +40,7 @@ struct WindowGradArgs {
   const void* dout;
   void *dq, *dk, *dv;
   Strides3 sdo, sdq, sdk, sdv;
-  float* delta;  // [B, Hq, Lq]: sum over the channels of dout * out
+  float* delta;  // a record per row [B, Hq, Lq]: fp32 the sum over the channels of dout * out; bf16 four floats (usv_window_grad.hip)
   // Key blocks are `block` keys.  Those below sink_blocks (every later row sees them) have sink_parts pieces, the others parts.
   int block, blocks, sink_blocks, sink_parts, parts;
   float* partial;  // dk, dv of the pieces: [slot][2][block][d]; a block in one piece has no slot
@@ -182,7 +182,8 @@ constexpr int kWindowRows = 64;  // query rows of a workgroup
 hipError_t launch_window_f32(const WindowArgs& a, int d, hipStream_t st);
 hipError_t launch_window_bf16(const WindowArgs& a, int d, hipStream_t st);
 hipError_t launch_window_join(const WindowArgs& a, bool bf16, int d, hipStream_t st);
-hipError_t launch_window_grad_f32(const WindowGradArgs& a, bool bf16, int d, hipStream_t st);
+hipError_t launch_window_grad_f32(const WindowGradArgs& a, int d, hipStream_t st);
+hipError_t launch_window_grad_bf16(const WindowGradArgs& a, int d, hipStream_t st);
 hipError_t launch_window_grad_join(const WindowGradArgs& a, bool bf16, int d, hipStream_t st);
 
 }  // namespace usv

@@ -428,13 +428,16 @@ hipError_t launch_window_join(const WindowArgs& a, bool bf16, int d, hipStream_t
   });
 }
 
-hipError_t launch_window_grad_f32(const WindowGradArgs& g, bool bf16, int d, hipStream_t st) {
+hipError_t launch_window_grad_f32(const WindowGradArgs& g, int d, hipStream_t st) {
   const unsigned q_grid = (unsigned)((g.f.w.Lq + kWindowRows - 1) / kWindowRows * g.f.w.B * g.f.w.Hq);
-  return by_type(bf16, d, [&](auto t, auto dc) {
+  auto go = [&](auto dc) {
     constexpr int D = decltype(dc)::value;
-    if (q_grid) window_grad_q<decltype(t), D><<<q_grid, 256, 0, st>>>(g);
-    if (g.blocks) window_grad_kv<decltype(t), D><<<window_pieces(g), 256, 0, st>>>(g);
-  });
+    if (q_grid) window_grad_q<float, D><<<q_grid, 256, 0, st>>>(g);
+    if (g.blocks) window_grad_kv<float, D><<<window_pieces(g), 256, 0, st>>>(g);
+  };
+  if (d == 128) go(std::integral_constant<int, 128>{});
+  else go(std::integral_constant<int, 64>{});
+  return hipGetLastError();
 }
 
 hipError_t launch_window_grad_join(const WindowGradArgs& g, bool bf16, int d, hipStream_t st) {

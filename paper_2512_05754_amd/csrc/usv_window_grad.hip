@@ -1,0 +1,435 @@
+// Gradients of windowed attention with sinks, bf16.
+//
+//   window_grad_q_bf16    a workgroup per 128 query rows of one head (32 a wave), walks their key list 64 keys at a time:
+//                         S^T = K Q^T, dP^T = V dout^T, dS^T = P^T (dP^T - D), dQ^T += K^T dS^T.  It also forms D = sum(dout * out) and leaves
+//                         {lse, D, lo, hi} of every row for the other kernel.
+//   window_grad_kv_bf16   a workgroup per 128 keys of one key head (32 a wave), walks the rows that see them 64 at a time, all query heads
+//                         of the key head in turn: S = Q K^T, dP = dout V^T, dV^T += dout^T P, dK^T += Q^T dS.
+// S and dP are formed in both: 7 products instead of 5, and in return every sum has one owner: no atomics, the same bits every time, no
+// memory that grows with the window.
+//
+// Matrix cores: v_mfma_f32_16x16x32_bf16, lane = (c, G), c = lane % 16, G = lane / 16.  The products are arranged so that the eight values of S (or dS)
+// a lane holds of its column are, as they stand, the eight contraction slots of the second product's operand; the other operand is
+// read transposed from the row-major tile with ds_read_b64_tr_b16.
+//
+// Tiles: 64 rows of two tensors (K and V, or Q and dout), lines of 128 bytes [line][row][128], global_load_lds_dwordx4 into one of two
+// stages while the other is worked on: one barrier a tile.  A row is read both ways, as 16-byte pieces of 16 rows and as 32-byte pieces of 8 rows
+// (transposed); chunk k of row i lies at k ^ f(i / 2 % 8), f(p) = 2 (p % 4) + p / 4, which keeps both free of bank conflicts.
+//
+// P and dS are rounded to bf16 for the second product, nothing else is; sums are fp32.
+#include "usv_attn_bf16.h"
+#include "usv_window.h"
+
+namespace usv {
+namespace {
+
+constexpr int kRows = 64;             // rows of a tile
+constexpr int kLine = kRows * 128;    // bytes of a line of all rows
+constexpr int kBlock128 = 128;        // rows (keys) of a workgroup, 32 a wave
+
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void dma_scalar(unsigned lds, unsigned long long base, unsigned offset) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(offset), "s"(base) : "memory");
+}
+__device__ __forceinline__ void dma_lane(unsigned lds, unsigned long long addr) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(addr) : "memory");
+}
+__device__ __forceinline__ unsigned long long uniform(unsigned long long x) {
+  return ((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)x);
+}
+__device__ __forceinline__ unsigned long long address(const void* p, const Strides3& s, int b, int h) {
+  return uniform(reinterpret_cast<unsigned long long>(p) + b * s.batch + h * s.head);
+}
+__device__ __forceinline__ const uint16_t* row_of(const void* p, const Strides3& s, int b, int h, long long row) {
+  return reinterpret_cast<const uint16_t*>(static_cast<const unsigned char*>(p) + b * s.batch + h * s.head + row * s.token);
+}
+__device__ __forceinline__ uint16_t* row_of(void* p, const Strides3& s, int b, int h, long long row) {
+  return reinterpret_cast<uint16_t*>(static_cast<unsigned char*>(p) + b * s.batch + h * s.head + row * s.token);
+}
+
+// This wave's share of a tile's requests: rows 16 wave .. + 15 of both tensors.
+template <int D>
+struct Tile {
+  static constexpr int LINES = D / 64, TENSOR = LINES * kLine, STAGE = 2 * TENSOR;
+  unsigned a_even, a_odd, b_even, b_odd;  // lane offsets in 8 rows
+  int wave, lane;
+  long long a_pitch, b_pitch;
+  __device__ __forceinline__ void init(int wave_, long long ap, long long bp) {
+    wave = wave_, lane = threadIdx.x & 63, a_pitch = ap, b_pitch = bp;
+    const unsigned chunk = ((lane & 7) ^ ((lane >> 4) << 1)) << 4;
+    a_even = (lane >> 3) * (unsigned)ap + chunk, a_odd = (lane >> 3) * (unsigned)ap + (chunk ^ 16);
+    b_even = (lane >> 3) * (unsigned)bp + chunk, b_odd = (lane >> 3) * (unsigned)bp + (chunk ^ 16);
+  }
+  // rows row .. row + 63 of both
+  __device__ __forceinline__ void load(unsigned lds, unsigned long long a, unsigned long long b, long long row) const {
+    const unsigned long long a0 = a + (row + 16 * wave) * a_pitch, b0 = b + (row + 16 * wave) * b_pitch;
+    const unsigned to = lds + 16 * wave * 128;
+#pragma unroll
+    for (int line = 0; line < LINES; ++line) {
+      dma_scalar(to + line * kLine, a0 + line * 128, a_even);
+      dma_scalar(to + line * kLine + 1024, a0 + 8 * a_pitch + line * 128, a_odd);
+    }
+#pragma unroll
+    for (int line = 0; line < LINES; ++line) {
+      dma_scalar(to + TENSOR + line * kLine, b0 + line * 128, b_even);
+      dma_scalar(to + TENSOR + line * kLine + 1024, b0 + 8 * b_pitch + line * 128, b_odd);
+    }
+  }
+  // a row of its own for every row of the tile
+  template <typename F>
+  __device__ __forceinline__ void load_rows(unsigned lds, unsigned long long a, unsigned long long b, F row_at) const {
+    const unsigned to = lds + 16 * wave * 128;
+#pragma unroll 1
+    for (int r = 0; r < 2; ++r) {
+      const long long row = row_at(16 * wave + 8 * r + (lane >> 3));
+      const unsigned chunk = ((lane & 7) ^ (((lane >> 4) << 1) | r)) << 4;
+#pragma unroll
+      for (int line = 0; line < LINES; ++line) {
+        dma_lane(to + line * kLine + 1024 * r, a + row * a_pitch + line * 128 + chunk);
+        dma_lane(to + TENSOR + line * kLine + 1024 * r, b + row * b_pitch + line * 128 + chunk);
+      }
+    }
+  }
+};
+
+// Fragment reads from a tensor of a tile: rows 32 sub + 16 m + c, channels 32 t + 8 G ..
+struct Lanes {
+  unsigned rows, columns;
+  __device__ __forceinline__ void init() {
+    const int lane = threadIdx.x & 63, c = lane & 15, G = lane >> 4;
+    rows = c * 128 + ((G ^ ((((c >> 1) & 3) << 1) | (c >> 3))) << 4);
+    const int row = 4 * G + (c >> 2), p = row >> 1;
+    columns = row * 128 + ((((c & 3) >> 1) ^ (((p & 3) << 1) | (p >> 2))) << 4) + (c & 1) * 8;
+  }
+  __device__ __forceinline__ bf16x8 row_frag(const unsigned char* tensor, int sub, int m, int t) const {
+    return *reinterpret_cast<const bf16x8*>(tensor + (rows ^ ((t & 1) << 6)) + (t >> 1) * kLine + (32 * sub + 16 * m) * 128);
+  }
+  // channels 16 dt + c as rows; slots 0..3: tile rows 32 sub + 4 G + (0..3), slots 4..7: 16 further
+  __device__ __forceinline__ bf16x8 column_frag(const unsigned char* tensor, int sub, int dt) const {
+    const unsigned char* p = tensor + (columns ^ ((dt & 3) << 5)) + (dt >> 2) * kLine + 32 * sub * 128;
+    const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)p);
+    const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)(p + 16 * 128));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+// s (quarter 2 m + nt: rows 16 m + 4 G .. of the tile's 32, columns 16 nt + c) = rows of the tensor times the lane's columns
+template <int D>
+__device__ __forceinline__ f32x16 rows_times(const unsigned char* tensor, const Lanes& at, int sub, const bf16x8 (&f)[2][D / 32]) {
+  f32x16 s;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const bf16x8 x = at.row_frag(tensor, sub, m, t);
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) {
+        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+        set_quarter(s, 2 * m + nt, __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, f[nt][t], t == 0 ? zero : quarter(s, 2 * m + nt), 0, 0, 0));
+      }
+    }
+  return s;
+}
+// o[nt][dt / 4] (quarter dt % 4: channels 16 dt + 4 G .., column 16 nt + c) += columns of the tensor times p
+template <int D>
+__device__ __forceinline__ void columns_times(const unsigned char* tensor, const Lanes& at, int sub, const bf16x8 (&p)[2], f32x16 (&o)[2][D / 64]) {
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) {
+    const bf16x8 x = at.column_frag(tensor, sub, dt);
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+      set_quarter(o[nt][dt >> 2], dt & 3, __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p[nt], quarter(o[nt][dt >> 2], dt & 3), 0, 0, 0));
+  }
+#pragma unroll
+  for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+    for (int x = 0; x < D / 64; ++x) asm volatile("" : "+v"(o[nt][x]));  // in place (see quarter())
+}
+template <int D>
+__device__ __forceinline__ void clear(f32x16 (&o)[2][D / 64]) {
+#pragma unroll
+  for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+    for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[nt][x][r] = 0.f;
+}
+
+template <int D, int WPS>
+__global__ __launch_bounds__(256, WPS) void window_grad_q_bf16(WindowGradArgs g) {
+  using T = Tile<D>;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * T::STAGE];
+  const WindowArgs& a = g.f;
+  const WindowSlot slot = window_slot(a.w, blockIdx.x, (a.w.Lq + kBlock128 - 1) / kBlock128);
+  const int hk = slot.h / a.w.group;
+  const WindowSeq seq = window_seq_of(a.w, slot.b);
+  WindowKeys keys = window_keys(a.w, seq, (long long)slot.blk * kBlock128, kBlock128);
+  window_uniform(&keys);
+  const int lane = threadIdx.x & 63, c = lane & 15, G = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tiles = (keys.count + kRows - 1) / kRows;
+  const unsigned long long ka = address(a.k, a.sk, slot.b, hk), va = address(a.v, a.sv, slot.b, hk);
+  const unsigned lds = lds_address(smem);
+  T tile;
+  tile.init(wave, a.sk.token, a.sv.token);
+  auto request = [&](int t) {
+    const int e = t * kRows;
+    const unsigned to = lds + (t & 1) * T::STAGE;
+    if (e + kRows <= keys.count && (e >= keys.head || e + kRows <= keys.head)) tile.load(to, ka, va, window_key(keys, e));
+    else tile.load_rows(to, ka, va, [&](int r) { return (long long)window_key(keys, min(e + r, keys.count - 1)); });
+  };
+  if (tiles > 0) request(0);
+
+  bf16x8 qf[2][D / 32], dof[2][D / 32];
+  float nlse[2], delta[2];
+  WindowRange range[2];
+  const int row0 = slot.blk * kBlock128 + 32 * wave;
+  if (tiles > 0) {
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      const int row = row0 + 16 * nt + c, some = min(max(row, keys.i0), keys.i1 - 1);
+      const long long id = ((long long)slot.b * a.w.Hq + slot.h) * a.w.Lq + some;
+      const uint16_t* qp = row_of(a.q, a.sq, slot.b, slot.h, some) + 8 * G;
+      const uint16_t* dp = row_of(g.dout, g.sdo, slot.b, slot.h, some) + 8 * G;
+      const uint16_t* op = row_of(static_cast<const void*>(a.out), a.so, slot.b, slot.h, some) + 8 * G;
+      float sum = 0.f;
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t) {
+        qf[nt][t] = *reinterpret_cast<const bf16x8*>(qp + 32 * t);
+        dof[nt][t] = *reinterpret_cast<const bf16x8*>(dp + 32 * t);
+        const bf16x8 of = *reinterpret_cast<const bf16x8*>(op + 32 * t);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = fmaf((float)dof[nt][t][e], (float)of[e], sum);
+      }
+      delta[nt] = sum_over_groups(sum);
+      nlse[nt] = -a.lse[id] * kLog2e;
+      range[nt] = window_range(a.w, seq.n, seq.first + some);
+      if (G == 0 && row == some)
+        reinterpret_cast<float4*>(g.delta)[id] = make_float4(nlse[nt], delta[nt], __int_as_float(range[nt].lo), __int_as_float(range[nt].hi));
+    }
+  }
+  f32x16 dq[2][D / 64];
+  clear<D>(dq);
+  Lanes at;
+  at.init();
+  const float sl = a.scale * kLog2e;
+  wait_vm<0>();
+#pragma unroll
+  for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) asm volatile("" : "+v"(qf[nt][t]), "+v"(dof[nt][t]));
+  for (int t = 0; t < tiles; ++t) {
+    wait_vm<0>();
+    __syncthreads();  // the tile is there; everybody is done with the other stage
+    if (t + 1 < tiles) request(t + 1);
+    const unsigned char* kt = smem + (t & 1) * T::STAGE;
+    const unsigned char* vt = kt + T::TENSOR;
+    const bool open = window_tile_open(keys, t * kRows, kRows);
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+      f32x16 s = rows_times<D>(kt, at, sub, qf);
+      if (!open) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int e = t * kRows + 32 * sub + 16 * m + 4 * G + r, key = window_key(keys, e);
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) s[4 * (2 * m + nt) + r] = (e < keys.count) & window_sees(range[nt], a.w.sink, key) ? s[4 * (2 * m + nt) + r] : -INFINITY;
+          }
+      }
+      const f32x16 dp = rows_times<D>(vt, at, sub, dof);
+      bf16x8 ds[2];
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int x = 4 * (2 * m + nt) + r;
+            ds[nt][4 * m + r] = (__bf16)(fast_exp2(fmaf(s[x], sl, nlse[nt])) * (dp[x] - delta[nt]));
+          }
+      columns_times<D>(kt, at, sub, ds, dq);
+    }
+  }
+#pragma unroll
+  for (int nt = 0; nt < 2; ++nt) {
+    const int row = row0 + 16 * nt + c;
+    if (row >= a.w.Lq) continue;
+    const bool live = row >= keys.i0 && row < keys.i1;
+    uint16_t* dst = row_of(g.dq, g.sdq, slot.b, slot.h, row) + 4 * G;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) {
+      const f32x4 x = quarter(dq[nt][dt >> 2], dt & 3);
+      store4<false>(dst + 16 * dt, live ? make_float4(x[0] * a.scale, x[1] * a.scale, x[2] * a.scale, x[3] * a.scale) : make_float4(0.f, 0.f, 0.f, 0.f), 0);
+    }
+  }
+}
+
+template <int D, int WPS>
+__global__ __launch_bounds__(256, WPS) void window_grad_kv_bf16(WindowGradArgs g) {
+  using T = Tile<D>;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * T::STAGE];
+  __shared__ __attribute__((aligned(16))) float4 srow[2][kRows];  // -lse (log2 domain), D, lo, hi of a row
+  const WindowArgs& a = g.f;
+  const WindowPiece pc = window_piece(g, blockIdx.x);
+  const int k0 = pc.block * kBlock128;
+  const WindowSeq seq = window_seq_of(a.w, pc.b);
+  const WindowRows rows = window_rows(a.w, seq, k0, kBlock128);
+  const int i0 = __builtin_amdgcn_readfirstlane(rows.i0), i1 = __builtin_amdgcn_readfirstlane(rows.i1);
+  const int lane = threadIdx.x & 63, c = lane & 15, G = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tiles = (i1 - i0 + kRows - 1) / kRows;
+  const long long all = (long long)tiles * a.w.group;
+  const int n0 = __builtin_amdgcn_readfirstlane((int)(all * pc.part / pc.parts)), n1 = __builtin_amdgcn_readfirstlane((int)(all * (pc.part + 1) / pc.parts));
+  f32x16 dk[2][D / 64], dv[2][D / 64];
+  clear<D>(dk);
+  clear<D>(dv);
+  if (n0 < n1) {
+    // rows [o0, o1) see every key of the block
+    int o0 = i0, o1 = i1;
+    {
+      const long long end = (long long)k0 + kBlock128;
+      if (end > seq.n) o1 = o0;
+      if (a.w.right >= 0) o0 = (int)min((long long)i1, max((long long)i0, ((end + a.w.chunk - 1) / a.w.chunk - a.w.right - 1) * a.w.chunk - seq.first));
+      if (a.w.left >= 0 && end > a.w.sink) o1 = (int)min((long long)o1, max((long long)i0, ((long long)k0 / a.w.chunk + a.w.left + 1) * a.w.chunk - seq.first));
+      o0 = __builtin_amdgcn_readfirstlane(o0), o1 = __builtin_amdgcn_readfirstlane(o1);
+    }
+    const unsigned lds = lds_address(smem), lds_row = lds_address(srow);
+    T tile;
+    tile.init(wave, a.sq.token, g.sdo.token);
+    auto request = [&](int h, int t, int stage) {
+      const int i = i0 + t * kRows;
+      const unsigned long long qa = address(a.q, a.sq, pc.b, h), da = address(g.dout, g.sdo, pc.b, h);
+      const unsigned to = lds + stage * T::STAGE;
+      if (i + kRows <= i1) tile.load(to, qa, da, i);
+      else tile.load_rows(to, qa, da, [&](int r) { return (long long)min(i + r, i1 - 1); });
+      if (wave == 0) {
+        const long long id = ((long long)pc.b * a.w.Hq + h) * a.w.Lq + min(i + lane, i1 - 1);
+        dma_lane(lds_row + stage * (kRows * 16), reinterpret_cast<unsigned long long>(reinterpret_cast<const float4*>(g.delta) + id));
+      }
+    };
+    int h = pc.h * a.w.group + n0 / tiles, t = n0 % tiles;
+    h = __builtin_amdgcn_readfirstlane(h), t = __builtin_amdgcn_readfirstlane(t);
+    request(h, t, 0);
+
+    bf16x8 kf[2][D / 32], vf[2][D / 32];
+    const int key0 = k0 + 32 * wave + c;
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      // (a key that nobody sees may hold anything: its lanes take zeros)
+      const WindowRows who = window_rows(a.w, seq, key0 + 16 * nt, 1);
+      const bool seen = who.i0 < who.i1;
+      const int key = seen ? key0 + 16 * nt : 0;
+      const uint16_t* kp = row_of(a.k, a.sk, pc.b, pc.h, key) + 8 * G;
+      const uint16_t* vp = row_of(a.v, a.sv, pc.b, pc.h, key) + 8 * G;
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x) {
+        const bf16x8 zero = {};
+        kf[nt][x] = seen ? *reinterpret_cast<const bf16x8*>(kp + 32 * x) : zero;
+        vf[nt][x] = seen ? *reinterpret_cast<const bf16x8*>(vp + 32 * x) : zero;
+      }
+    }
+    Lanes at;
+    at.init();
+    const float sl = a.scale * kLog2e;
+    wait_vm<0>();
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x) asm volatile("" : "+v"(kf[nt][x]), "+v"(vf[nt][x]));
+    for (int n = n0; n < n1; ++n) {
+      wait_vm<0>();
+      __syncthreads();
+      const int i = i0 + t * kRows, stage = (n - n0) & 1;
+      if (++t == tiles) t = 0, ++h;
+      if (n + 1 < n1) request(h, t, stage ^ 1);
+      const unsigned char* qt = smem + stage * T::STAGE;
+      const unsigned char* dt = qt + T::TENSOR;
+      const bool open = i >= o0 && i + kRows <= o1;
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        f32x16 s = rows_times<D>(qt, at, sub, kf);
+        if (!open) {
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int x = 32 * sub + 16 * m + 4 * G + r;
+              const float4 rec = srow[stage][x];
+              const WindowRange range = {__float_as_int(rec.z), i + x < i1 ? __float_as_int(rec.w) : 0};
+#pragma unroll
+              for (int nt = 0; nt < 2; ++nt) s[4 * (2 * m + nt) + r] = window_sees(range, a.w.sink, key0 + 16 * nt) ? s[4 * (2 * m + nt) + r] : -INFINITY;
+            }
+        }
+        float del[2][4];
+        bf16x8 p[2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float2 rec = *reinterpret_cast<const float2*>(&srow[stage][32 * sub + 16 * m + 4 * G + r]);
+            del[m][r] = rec.y;
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) {
+              const int x = 4 * (2 * m + nt) + r;
+              s[x] = fast_exp2(fmaf(s[x], sl, rec.x));
+              p[nt][4 * m + r] = (__bf16)s[x];
+            }
+          }
+        columns_times<D>(dt, at, sub, p, dv);
+        const f32x16 dp = rows_times<D>(dt, at, sub, vf);
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int x = 4 * (2 * m + nt) + r;
+              p[nt][4 * m + r] = (__bf16)(s[x] * (dp[x] - del[m][r]));
+            }
+        columns_times<D>(qt, at, sub, p, dk);
+      }
+    }
+  }
+  const int key0 = k0 + 32 * wave + c;
+#pragma unroll
+  for (int nt = 0; nt < 2; ++nt) {
+    const int key = key0 + 16 * nt;
+    if (pc.slot >= 0) {
+      float* dst = g.partial + pc.slot * (2LL * kBlock128 * D) + (32 * wave + 16 * nt + c) * D + 4 * G;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) {
+        const f32x4 x = quarter(dk[nt][dt >> 2], dt & 3), y = quarter(dv[nt][dt >> 2], dt & 3);
+        store4<true>(dst + 16 * dt, make_float4(x[0], x[1], x[2], x[3]), 0);
+        store4<true>(dst + kBlock128 * D + 16 * dt, make_float4(y[0], y[1], y[2], y[3]), 0);
+      }
+    } else if (key < a.w.Lk) {
+      uint16_t* pk = row_of(g.dk, g.sdk, pc.b, pc.h, key) + 4 * G;
+      uint16_t* pv = row_of(g.dv, g.sdv, pc.b, pc.h, key) + 4 * G;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) {
+        const f32x4 x = quarter(dk[nt][dt >> 2], dt & 3), y = quarter(dv[nt][dt >> 2], dt & 3);
+        store4<false>(pk + 16 * dt, make_float4(x[0] * a.scale, x[1] * a.scale, x[2] * a.scale, x[3] * a.scale), 0);
+        store4<false>(pv + 16 * dt, make_float4(y[0], y[1], y[2], y[3]), 0);
+      }
+    }
+  }
+}
+
+template <int D, int WPS>
+hipError_t run(const WindowGradArgs& g, hipStream_t st) {
+  const unsigned q_grid = (unsigned)((g.f.w.Lq + kBlock128 - 1) / kBlock128 * g.f.w.B * g.f.w.Hq);
+  if (q_grid) window_grad_q_bf16<D, WPS><<<q_grid, 256, 0, st>>>(g);
+  if (g.blocks) window_grad_kv_bf16<D, WPS><<<window_pieces(g), 256, 0, st>>>(g);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_window_grad_bf16(const WindowGradArgs& g, int d, hipStream_t st) { return d == 128 ? run<128, 2>(g, st) : run<64, 3>(g, st); }
+
+}  // namespace usv
