@@ -30,6 +30,7 @@ struct CacheAttnArgs {
   CacheShape c;
   const unsigned char* cache;
   WindowArgs f;  // q, out, lse, pieces; k, v unused
+  unsigned div_mul, div_shift;  // x / (page_size / 16) = (mulhi(x, div_mul) + x) >> div_shift, x < 2^27
 };
 
 constexpr int kCacheGroup = 16;  // keys of a page that are looked up together; page_size is a multiple

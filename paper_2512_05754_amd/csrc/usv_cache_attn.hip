@@ -58,12 +58,35 @@ struct Raw {  // one lane's share of a key (or value) row
   }
 };
 
+template <int NT>
+struct Logits {  // quarter nt of s[m]
+  f32x16 s[2];
+  __device__ __forceinline__ f32x4 get(int m, int nt) const { return quarter(s[m], nt); }
+  __device__ __forceinline__ void set(int m, int nt, const f32x4& x) { set_quarter(s[m], nt, x); }
+  __device__ __forceinline__ float at(int m, int nt, int r) const { return s[m][4 * nt + r]; }
+  __device__ __forceinline__ void put(int m, int nt, int r, float x) { s[m][4 * nt + r] = x; }
+};
+template <>
+struct Logits<1> {
+  f32x4 s[2];
+  __device__ __forceinline__ f32x4 get(int m, int) const { return s[m]; }
+  __device__ __forceinline__ void set(int m, int, const f32x4& x) { s[m] = x; }
+  __device__ __forceinline__ float at(int m, int, int r) const { return s[m][r]; }
+  __device__ __forceinline__ void put(int m, int, int r, float x) { s[m][r] = x; }
+};
+__device__ __forceinline__ const unsigned char* uniform(const unsigned char* p) {
+  const unsigned long long x = reinterpret_cast<unsigned long long>(p);
+  return reinterpret_cast<const unsigned char*>(((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)x));
+}
+
 template <int D, int BITS, int NT>
 __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void cache_attn(CacheAttnArgs a, int row_tiles) {
   constexpr int ROWS = 16 * NT, KS = D / 32, DT = D / 16, OT = DT / 4, CB = D * BITS / 8, SB = D / 32;
   constexpr int PITCH = D * 2 + 16, AREA = 32 * PITCH, OPITCH = D + 4;
+  constexpr bool QLDS = NT == 4;  // there are no registers for 64 rows of Q: read back from LDS, each fragment for two products
   static_assert(16 * OPITCH * 4 <= AREA, "a wave's result of 16 rows fits where its V rows were");
   __shared__ __attribute__((aligned(16))) unsigned char smem[4 * AREA];
+  __shared__ __attribute__((aligned(16))) unsigned char q_lds[QLDS ? NT * KS * 1024 : 16];
   __shared__ int2 srange[ROWS];
   __shared__ float sref[4][ROWS], ssum[4][ROWS];
   const WindowShape& w = a.f.w;
@@ -73,26 +96,49 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void cache_attn(CacheAttnArgs
   const WindowSeq seq = window_seq_of(w, b);
   const int all_rows = w.Lq * w.group, row0 = tile * ROWS, row1 = min(row0 + ROWS, all_rows);
   const int i0 = row0 / w.group, i1 = (row1 - 1) / w.group + 1;  // query tokens
-  const WindowKeys keys = window_keys(w, seq, i0, i1 - i0);
+  WindowKeys keys = window_keys(w, seq, i0, i1 - i0);
+  window_uniform(&keys);
   // groups of 16 keys: list entry x is group x where x < head_groups, else x + skip_groups
   const int lo = keys.head + keys.skip, hi = keys.count + keys.skip;
   const int head_groups = (keys.head + kCacheGroup - 1) / kCacheGroup;
   const int skip_groups = max(0, lo / kCacheGroup - head_groups);
   const int groups = keys.count > 0 ? (hi + kCacheGroup - 1) / kCacheGroup - skip_groups : 0;
   const int steps = (groups + 1) / 2;
-  const int s0 = (int)((long long)steps * blockIdx.y / a.f.splits), s1 = (int)((long long)steps * (blockIdx.y + 1) / a.f.splits);
+  const int s0 = __builtin_amdgcn_readfirstlane((int)((long long)steps * blockIdx.y / a.f.splits));
+  const int s1 = __builtin_amdgcn_readfirstlane((int)((long long)steps * (blockIdx.y + 1) / a.f.splits));
+
+  const int32_t* const table = a.c.table + (long long)b * a.c.table_pages;
+  unsigned char* const area = smem + wave * AREA;
+  auto group_of = [&](int x) { return x < head_groups ? x : x + skip_groups; };
+  auto slot_of = [&](unsigned g) { return (__umulhi(g, a.div_mul) + g) >> a.div_shift; };
+  // Pages of this wave's next 32 steps: lane 2 k + m holds that of group m of step first + 4 k.
+  int pages_v = 0;
+  auto look_up = [&](int first) {
+    const int x = min(2 * (first + 4 * (lane >> 1)) + (lane & 1), groups - 1);
+    pages_v = min(max(table[slot_of(group_of(x))], 0), a.c.pages - 1);
+  };
+  const int step0 = s0 + wave;
+  if (step0 < s1) look_up(step0);
 
   for (int r = threadIdx.x; r < ROWS; r += 256) {
     const WindowRange x = row0 + r < row1 ? window_range(w, seq.n, seq.first + (row0 + r) / w.group) : WindowRange{0, 0};
     srange[r] = make_int2(x.lo, x.hi);
   }
-  bf16x8 qf[NT][KS];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
+  // Q fragments: lane (c, G) has row 16 nt + c, channels D / 4 * G + 8 t .. + 8
+  auto load_q = [&](int nt, int t) {
     const int row = min(row0 + 16 * nt + c, row1 - 1), i = row / w.group, h = hk * w.group + row % w.group;
-    const uint16_t* p = reinterpret_cast<const uint16_t*>(static_cast<const unsigned char*>(a.f.q) + b * a.f.sq.batch + h * a.f.sq.head + i * a.f.sq.token) + D / 4 * G;
+    const unsigned char* p = static_cast<const unsigned char*>(a.f.q) + b * a.f.sq.batch + h * a.f.sq.head + i * a.f.sq.token;
+    return *reinterpret_cast<const bf16x8*>(p + (D / 4 * G + 8 * t) * 2);
+  };
+  bf16x8 qf[QLDS ? 1 : NT][KS];
+  if constexpr (QLDS) {
 #pragma unroll
-    for (int t = 0; t < KS; ++t) qf[nt][t] = *reinterpret_cast<const bf16x8*>(p + 8 * t);
+    for (int t = 0; t < KS; ++t) *reinterpret_cast<bf16x8*>(q_lds + ((wave * KS + t) * 64 + lane) * 16) = load_q(wave, t);  // (NT = 4: a wave, a row tile)
+  } else {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int t = 0; t < KS; ++t) qf[nt][t] = load_q(nt, t);
   }
   f32x16 o[NT][OT];
   float nm[NT], l[NT];
@@ -108,56 +154,65 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void cache_attn(CacheAttnArgs
 
   const float sl = a.f.scale * kLog2e;
   const int page_groups = a.c.page_size / kCacheGroup;
-  const long long head_bytes = a.c.head_bytes();
-  const int32_t* table = a.c.table + (long long)b * a.c.table_pages;
-  unsigned char* const area = smem + wave * AREA;
+  const unsigned head_bytes = (unsigned)a.c.head_bytes(), v_codes = a.c.page_size * CB, scales = 2 * v_codes, v_scales = a.c.page_size * SB;
   Raw<D, BITS> kr[2], vr[2];
-  auto group_of = [&](int x) { return x < head_groups ? x : x + skip_groups; };
-  // The rows of a group that no row of the workgroup sees are not touched: their lanes take one that is seen.
-  auto fetch = [&](int step) {
+  // k: this step's place in pages_v.  The rows of a group that no row of the workgroup sees are not touched: their lanes take one that is seen.
+  auto fetch = [&](int step, int k) {
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      const int g = group_of(min(2 * step + m, groups - 1));
-      const int slot = g / page_groups, first = (g - slot * page_groups) * kCacheGroup;
-      const int page = min(max(__builtin_amdgcn_readfirstlane(table[slot]), 0), a.c.pages - 1);
-      const unsigned char* base = a.cache + ((long long)page * w.Hkv + hk) * head_bytes;
-      const int j = g * kCacheGroup + c, some = g < head_groups ? g * kCacheGroup : max(g * kCacheGroup, lo);
-      const bool seen = j < hi && (j < keys.head || j >= lo);
-      const int row = first + (seen ? c : some - g * kCacheGroup);
-      const unsigned char* codes = base + (long long)row * CB + CB / 4 * G;
-      const unsigned char* scales = base + 2LL * a.c.page_size * CB + row * SB + (D == 128 ? G : G >> 1);
-      kr[m].load(codes, scales);
-      vr[m].load(codes + (long long)a.c.page_size * CB, scales + a.c.page_size * SB);
+      const int g = __builtin_amdgcn_readfirstlane(group_of(min(2 * step + m, groups - 1)));
+      const int page = __builtin_amdgcn_readlane(pages_v, 2 * k + m);
+      const int first = __builtin_amdgcn_readfirstlane((g - (int)slot_of(g) * page_groups) * kCacheGroup);
+      const unsigned char* base = uniform(a.cache + ((unsigned long long)page * w.Hkv + hk) * head_bytes);
+      int row = c;
+      const int j0 = g * kCacheGroup;
+      if (j0 + kCacheGroup > hi || (j0 < lo && j0 + kCacheGroup > keys.head)) {
+        const int j = j0 + c;
+        row = (j < hi) & ((j < keys.head) | (j >= lo)) ? c : g < head_groups ? 0 : max(0, lo - j0);
+      }
+      const unsigned codes = row * CB + CB / 4 * G, scale = row * SB + (D == 128 ? G : G >> 1);
+      const unsigned char* at_codes = base + first * CB;
+      const unsigned char* at_scales = base + scales + first * SB;
+      kr[m].load(at_codes + codes, at_scales + scale);
+      vr[m].load(at_codes + v_codes + codes, at_scales + v_scales + scale);
     }
   };
-  int step = s0 + wave;
-  if (step < s1) fetch(step);
-  for (; step < s1; step += 4) {
-    bf16x8 kf[2][KS];
-    bf16x8 vf[2][KS];
+  if (step0 < s1) fetch(step0, 0);
+  int k = 0;
+  for (int step = step0; step < s1; step += 4) {
+    // ---- V to LDS, S^T = K Q^T: quarter nt of s[m]: key 16 m + 4 G + r of the step, row 16 nt + c
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      const float fk = kr[m].factor(), fv = vr[m].factor();
+      const float f = vr[m].factor();
 #pragma unroll
-      for (int t = 0; t < KS; ++t) kf[m][t] = kr[m].eight(t, fk), vf[m][t] = vr[m].eight(t, fv);
+      for (int t = 0; t < KS; ++t) *reinterpret_cast<bf16x8*>(area + (16 * m + c) * PITCH + (D / 4 * G + 8 * t) * 2) = vr[m].eight(t, f);
     }
-    if (step + 4 < s1) fetch(step + 4);
+    Logits<NT> s;
+    {
+      const float f0 = kr[0].factor(), f1 = kr[1].factor();
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+      for (int t = 0; t < KS; ++t) {
+        const bf16x8 k0 = kr[0].eight(t, f0), k1 = kr[1].eight(t, f1);
 #pragma unroll
-      for (int t = 0; t < KS; ++t) *reinterpret_cast<bf16x8*>(area + (16 * m + c) * PITCH + (D / 4 * G + 8 * t) * 2) = vf[m][t];
-    // ---- S^T: s[m][4 nt + r]: key 16 m + 4 G + r of the step, row 16 nt + c
-    float s[2][4 * NT];
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int t = 0; t < KS; ++t) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[m][t], qf[nt][t], x, 0, 0, 0);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s[m][4 * nt + r] = x[r];
+        for (int nt = 0; nt < NT; ++nt) {
+          const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+          bf16x8 q;
+          if constexpr (QLDS) q = *reinterpret_cast<const bf16x8*>(q_lds + ((nt * KS + t) * 64 + lane) * 16);
+          else q = qf[nt][t];
+          s.set(0, nt, __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q, t == 0 ? zero : s.get(0, nt), 0, 0, 0));
+          s.set(1, nt, __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q, t == 0 ? zero : s.get(1, nt), 0, 0, 0));
+        }
       }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (step + 4 < s1) {  // (what was held of this step has been converted)
+      if (++k == 32) {
+        k = 0;
+        look_up(step + 4);
+      }
+      fetch(step + 4, k);
+    }
+    __builtin_amdgcn_sched_barrier(0);
     bool open = true;
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
@@ -173,7 +228,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void cache_attn(CacheAttnArgs
         for (int m = 0; m < 2; ++m) {
           const int x = 2 * step + m, j0 = group_of(x) * kCacheGroup + 4 * G;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) s[m][4 * nt + r] = x < groups && window_sees(range, w.sink, j0 + r) ? s[m][4 * nt + r] : -INFINITY;
+          for (int r = 0; r < 4; ++r) s.put(m, nt, r, (x < groups) & window_sees(range, w.sink, j0 + r) ? s.at(m, nt, r) : -INFINITY);
         }
       }
     }
@@ -181,7 +236,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void cache_attn(CacheAttnArgs
     float mx[NT], over = -INFINITY;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      mx[nt] = max8(s[0][4 * nt], s[0][4 * nt + 1], s[0][4 * nt + 2], s[0][4 * nt + 3], s[1][4 * nt], s[1][4 * nt + 1], s[1][4 * nt + 2], s[1][4 * nt + 3]);
+      mx[nt] = max8(s.at(0, nt, 0), s.at(0, nt, 1), s.at(0, nt, 2), s.at(0, nt, 3), s.at(1, nt, 0), s.at(1, nt, 1), s.at(1, nt, 2), s.at(1, nt, 3));
       over = fmaxf(over, fmaf(mx[nt], sl, nm[nt]));
     }
     if (__any(over > kRescaleSlack)) {
@@ -204,7 +259,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void cache_attn(CacheAttnArgs
       for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float p = fast_exp2(fmaf(s[m][4 * nt + r], sl, nm[nt]));
+          const float p = fast_exp2(fmaf(s.at(m, nt, r), sl, nm[nt]));
           l[nt] += p;
           pf[nt][4 * m + r] = (__bf16)p;
         }
@@ -289,8 +344,13 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void cache_attn(CacheAttnArgs
 
 }  // namespace
 
-hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t st) {
-  const WindowShape& w = a.f.w;
+hipError_t launch_cache_attn(const CacheAttnArgs& args, hipStream_t st) {
+  const WindowShape& w = args.f.w;
+  CacheAttnArgs a = args;
+  const unsigned n = a.c.page_size / kCacheGroup;
+  a.div_shift = 0;
+  while ((1u << a.div_shift) < n) ++a.div_shift;
+  a.div_mul = (unsigned)(((1ull << 32) * ((1ull << a.div_shift) - n)) / n + 1);
   const int rows = cache_attn_rows(w), tiles = (w.Lq * w.group + rows - 1) / rows;
   const dim3 grid((unsigned)(tiles * w.B * w.Hkv), a.f.splits);
   auto go = [&](auto d, auto bits) {
