@@ -14,7 +14,7 @@
 // of the next step.  The 16-byte chunks of a line are XOR-permuted on the global side so that K reads and transposing V reads are free of
 // bank conflicts.
 //
-// Addresses: a step whose 32 entries are neighbouring keys (all but the one that joins the sinks to the window and the last one) is
+// Addresses: a step whose 32 entries are neighbouring keys (all but the first and the one that joins the sinks to the window) is
 // fetched from scalar row addresses that move on by a constant, with fixed lane offsets: no vector instruction for any stride.  The
 // other steps compute a full address per lane.
 //
@@ -61,19 +61,21 @@ __device__ __forceinline__ unsigned long long uniform(unsigned long long x) {
   return ((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)x);
 }
 
-// The arguments, read again where they are asked for: kept over the loop they are scalar registers that it has not got.
-__device__ __forceinline__ const WindowArgs& again(const WindowArgs& a) {
-  unsigned long long p = reinterpret_cast<unsigned long long>(__builtin_amdgcn_kernarg_segment_ptr());
+// The arguments, read again (scalar loads) where they are asked for: kept over the loop they are registers that it has not got.
+typedef const __attribute__((address_space(4))) WindowArgs* ArgsAgain;
+__device__ __forceinline__ ArgsAgain again() {
+  ArgsAgain p = (ArgsAgain)__builtin_amdgcn_kernarg_segment_ptr();
   asm volatile("" : "+s"(p));
-  return *reinterpret_cast<const WindowArgs*>(p);
+  return p;
 }
 
-template <int D, int WPS, int QL_>
+// QL: Q fragments of the last channel step that are read back from LDS, four more reads a step.  All of Q in registers is 1 to 2 % faster where
+// every step is hot, but the other steps then spill: 480p frames, left 6, 1.94 ms against 2.05 (QL = 2: 1.99); d = 64, window 1000, 97.3 against 102.9 us.
+template <int D, int WPS, int QL>
 __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   constexpr int KS = D / 32, DT = D / 16, OT = (DT + 3) / 4;
   constexpr int LINES = D / 64, IPS = 2 * LINES;
   constexpr int KF = 3, VF = 2;  // fragments of K, V in flight
-  constexpr int QL = QL_;        // Q fragments of the last channel step that are read back from LDS: there are no registers for them
   constexpr int XROWS = DT * 8 + 4;
   constexpr int OSTRIDE = D + 4;
   constexpr int kWaveBytes = IPS * kItem > XROWS * 256 ? IPS * kItem : XROWS * 256;  // items, later the exchange area
@@ -84,7 +86,8 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   __shared__ __attribute__((aligned(16))) unsigned char q_tail[QL > 0 ? QL * 1024 : 16];
 
   const WindowShape& w = a.w;
-  const WindowSlot slot = window_slot(w, blockIdx.x, (w.Lq + kWindowRows - 1) / kWindowRows);
+  WindowSlot slot = window_slot(w, blockIdx.x, (w.Lq + kWindowRows - 1) / kWindowRows);
+  slot.blk = __builtin_amdgcn_readfirstlane(slot.blk), slot.b = __builtin_amdgcn_readfirstlane(slot.b), slot.h = __builtin_amdgcn_readfirstlane(slot.h);
   const WindowSeq seq = window_seq_of(w, slot.b);
   const int row0 = slot.blk * kWindowRows;
   WindowKeys keys = window_keys(w, seq, row0, kWindowRows);
@@ -92,11 +95,12 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   const int lane = threadIdx.x & 63, c16 = lane & 15, G = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  // entries of this workgroup: tiles of 64; this wave's steps are at first + 64 n
+  // Entries of this workgroup: tiles of 64 that end where the list does; what is missing from a whole number of them is missing ahead of
+  // entry 0, in the tile that is waited for anyway.  This wave's steps are at first + 64 n.
   const int tiles = (keys.count + 63) / 64;
-  const int t0 = (int)((long long)tiles * blockIdx.y / a.splits), t1 = (int)((long long)tiles * (blockIdx.y + 1) / a.splits);
-  const int first = t0 * 64 + wave * kStep, end = min(t1 * 64, keys.count);
-  const int n_steps = __builtin_amdgcn_readfirstlane(first < end ? (end - first + 63) / 64 : 0);
+  const int t0 = __builtin_amdgcn_readfirstlane((int)((long long)tiles * blockIdx.y / a.splits));
+  const int n_steps = __builtin_amdgcn_readfirstlane((int)((long long)tiles * (blockIdx.y + 1) / a.splits)) - t0;
+  const int first = keys.count - (tiles - t0) * 64 + wave * kStep;
 
   if (threadIdx.x < kWindowRows) {
     const int row = row0 + threadIdx.x;
@@ -104,7 +108,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
     srange[threadIdx.x] = make_int2(r.lo, r.hi);
   }
 
-  const int hk = slot.h / w.group;
+  const int hk = __builtin_amdgcn_readfirstlane(slot.h / w.group);
   const unsigned wave_lds = lds_address(smem) + wave * kWaveBytes;
   // DMA lane -> row lane / 8 of an instruction's 8 rows, 16-byte chunk lane % 8 of the line; K chunks are stored at chunk ^ (row / 2 % 8), V
   // chunks at chunk ^ 2 (row / 2 % 4)
@@ -115,17 +119,17 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   unsigned long long kb[4], vb[4];
   auto point_at = [&](int entry) {
     const long long key = window_key(keys, entry);
-    const WindowArgs& b = again(a);
-    const unsigned long long kb0 = reinterpret_cast<unsigned long long>(b.k) + slot.b * b.sk.batch + hk * b.sk.head;
-    const unsigned long long vb0 = reinterpret_cast<unsigned long long>(b.v) + slot.b * b.sv.batch + hk * b.sv.head;
+    const ArgsAgain b = again();
+    const unsigned long long kb0 = reinterpret_cast<unsigned long long>(b->k) + slot.b * b->sk.batch + hk * b->sk.head;
+    const unsigned long long vb0 = reinterpret_cast<unsigned long long>(b->v) + slot.b * b->sv.batch + hk * b->sv.head;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      kb[r] = uniform(kb0 + (key + 8 * r) * b.sk.token - 1024 * r);
-      vb[r] = uniform(vb0 + (key + 8 * r) * b.sv.token - 1024 * r);
+      kb[r] = uniform(kb0 + (key + 8 * r) * b->sk.token - 1024 * r);
+      vb[r] = uniform(vb0 + (key + 8 * r) * b->sv.token - 1024 * r);
     }
   };
   const unsigned long long kmove = uniform(64ull * a.sk.token), vmove = uniform(64ull * a.sv.token);
-  auto plain_step = [&](int e) { return e + kStep <= keys.count && (e >= keys.head || e + kStep <= keys.head); };
+  auto plain_step = [&](int e) { return e >= keys.head || (e >= 0 && e + kStep <= keys.head); };
   // item x of the step that kb, vb point at
   auto dma = [&](auto x_c) {
     constexpr int x = decltype(x_c)::value, LINE = x % LINES;
@@ -133,21 +137,21 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
     if constexpr (x < LINES) dma_rows<LINE>(lds, kb, k_even, k_odd);
     else dma_rows<LINE>(lds, vb, v_all, v_all);
   };
-  // all items of any step; entries past the list's end take its last key (the mask takes them out)
+  // all items of any step; entries ahead of the list take its first key (the mask takes them out)
   auto dma_step = [&](int e) {
     int ln = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
     asm volatile("" : "+v"(ln));  // formed here, on the rare path
-    const WindowArgs& b = again(a);
-    const unsigned long long kb0 = reinterpret_cast<unsigned long long>(b.k) + slot.b * b.sk.batch + hk * b.sk.head;
-    const unsigned long long vb0 = reinterpret_cast<unsigned long long>(b.v) + slot.b * b.sv.batch + hk * b.sv.head;
+    const ArgsAgain b = again();
+    const unsigned long long kb0 = reinterpret_cast<unsigned long long>(b->k) + slot.b * b->sk.batch + hk * b->sk.head;
+    const unsigned long long vb0 = reinterpret_cast<unsigned long long>(b->v) + slot.b * b->sv.batch + hk * b->sv.head;
 #pragma unroll 1
     for (int r = 0; r < 4; ++r) {
-      const long long key = window_key(keys, min(e + 8 * r + (ln >> 3), keys.count - 1));
+      const long long key = window_key(keys, max(e + 8 * r + (ln >> 3), 0));
       const unsigned kc = ((ln & 7) ^ (((4 * r) & 7) ^ (ln >> 4))) << 4, vc = ((ln & 7) ^ (((ln >> 4) & 3) << 1)) << 4;
 #pragma unroll
       for (int line = 0; line < LINES; ++line) {
-        dma_lane(wave_lds + line * kItem + 1024 * r, kb0 + key * b.sk.token + line * 128 + kc);
-        dma_lane(wave_lds + (LINES + line) * kItem + 1024 * r, vb0 + key * b.sv.token + line * 128 + vc);
+        dma_lane(wave_lds + line * kItem + 1024 * r, kb0 + key * b->sk.token + line * 128 + kc);
+        dma_lane(wave_lds + (LINES + line) * kItem + 1024 * r, vb0 + key * b->sv.token + line * 128 + vc);
       }
     }
   };
@@ -211,17 +215,19 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
     for (int t = 0; t < KS; ++t)
       if (t < KS - 1 || nt < 4 - QL) asm volatile("" : "+v"(qf[nt][t]));  // (else their loads sink into the loop, with waits for all memory)
 
-  // One step.  The next one is fetched item by item while this one is worked on, if it is of the plain kind; else all of it behind this one.
-  auto step = [&](int n) {
+  // One step.  HOT: every row sees all its keys, and the next step lies 64 keys further on; that one is fetched item by item while this one
+  // is worked on.  Otherwise (a few steps of a list: its ends and the diagonal) the mask is applied, and the next step is fetched behind this one if
+  // its rows need addresses of their own.
+  auto step = [&](auto hot_c, int n) {
+    constexpr bool HOT = decltype(hot_c)::value;
     const int e0 = first + 64 * n, e1 = e0 + 64;
-    const bool more = n + 1 < n_steps, ahead = more && plain_step(e1);
-    if (!ahead) {
-      wait_vm<0>();
-    } else if (e0 >= keys.head || e1 < keys.head) {  // on in the same stretch
+    const bool more = HOT || n + 1 < n_steps, ahead = HOT || (more && plain_step(e1));
+    if constexpr (HOT) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) kb[r] += kmove, vb[r] += vmove;
     } else {
-      point_at(e1);
+      if (ahead) point_at(e1);
+      else wait_vm<0>();
     }
     // Item x of this step is in LDS.  Younger requests: the items behind it and those of the next step asked for by then (none: nothing is
     // under way any more).
@@ -272,7 +278,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
     }
 
     // s[mt][4 nt + r] is entry e0 + 16 mt + 4 G + r, query 16 nt + c16
-    if (!window_tile_open(keys, e0, kStep)) {
+    if (!HOT && (e0 < 0 || !window_tile_open(keys, e0, kStep))) {
       int ln = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
       asm volatile("" : "+v"(ln));
 #pragma unroll
@@ -284,7 +290,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int e = e0 + 16 * mt + 4 * (ln >> 4) + r;
-            s[mt][4 * nt + r] = (e < keys.count) & window_sees(range, w.sink, window_key(keys, e)) ? s[mt][4 * nt + r] : -INFINITY;
+            s[mt][4 * nt + r] = (e >= 0) & window_sees(range, w.sink, window_key(keys, e)) ? s[mt][4 * nt + r] : -INFINITY;
           }
       }
     }
@@ -355,14 +361,28 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
     for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
       for (int x = 0; x < OT; ++x) asm volatile("" : "+v"(o[nt][x]));
-    if (more && !ahead) {
+    if (!HOT && more && !ahead) {
       wait_lds<0>();
       dma_step(e1);
       point_at(e1);
     }
   };
-  for (int n = 0; n < n_steps; ++n) step(n);
-  const WindowArgs& z = again(a);
+  // hot steps in a row from step n on
+  auto hot_steps = [&](int n) {
+    const int e0 = first + 64 * n, key = window_key(keys, e0);
+    if (e0 < 0 || (key < keys.all_lo && key >= keys.all_sink)) return 0;
+    const int open = e0 < keys.head || key < keys.all_lo ? keys.all_sink : keys.all_hi;  // (keys below are seen by every row)
+    int k = min(n_steps - 1 - n, (open - key + kStep) / 64);                               // the step's keys lie below
+    if (e0 < keys.head) k = min(k, (keys.head - e0 - kStep) / 64);                         // the next step's too
+    return max(k, 0);
+  };
+  for (int n = 0; n < n_steps;) {
+    const int until = n + __builtin_amdgcn_readfirstlane(hot_steps(n));
+    for (; n < until; ++n) step(std::true_type{}, n);
+    step(std::false_type{}, n);
+    ++n;
+  }
+  const ArgsAgain z = again();
 
   // ---- merge the two waves, stage the rows in LDS, store ----
   // Wave w finishes query tiles 2 w and 2 w + 1: it gives the other two away through its own area (dead by now), adds what the other wave
@@ -383,8 +403,8 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
       dst[(DT * 8 + 2 + e) * 64] = l_row[F + e];
     }
   };
-  const long long rows = (long long)z.w.B * z.w.Hq * z.w.Lq, id0 = ((long long)slot.b * z.w.Hq + slot.h) * z.w.Lq;
-  const bool parts = z.splits > 1;
+  const long long rows = (long long)z->w.B * z->w.Hq * z->w.Lq, id0 = ((long long)slot.b * z->w.Hq + slot.h) * z->w.Lq;
+  const bool parts = z->splits > 1;
   auto take = [&](auto first_c) {
     constexpr int F = decltype(first_c)::value;
     float* area = reinterpret_cast<float*>(smem + (wave ^ 1) * kWaveBytes);
@@ -406,10 +426,10 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
           const float val = o[F + e][dt >> 2][4 * (dt & 3) + r] * w0 + src[((e * DT + dt) * 4 + r) * 64] * w1;
           o[F + e][dt >> 2][4 * (dt & 3) + r] = live ? val : 0.f;
         }
-      if (G == 0 && row < z.w.Lq) {
+      if (G == 0 && row < z->w.Lq) {
         const float val = live ? (__log2f(lt) - ref) * kLn2 : -INFINITY;
-        if (parts) z.part_lse[blockIdx.y * rows + id0 + row] = val;
-        else if (z.lse) z.lse[id0 + row] = val;
+        if (parts) z->part_lse[blockIdx.y * rows + id0 + row] = val;
+        else if (z->lse) z->lse[id0 + row] = val;
       }
     }
     wait_lds<0>();  // every exchange value of this wave is in registers before its area is overwritten
@@ -431,14 +451,14 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   if (wave == 0) take(I0{});
   else take(I2{});
   const float* other = reinterpret_cast<const float*>(smem + (wave ^ 1) * kWaveBytes);
-  unsigned char* const dst = static_cast<unsigned char*>(z.out) + slot.b * z.so.batch + slot.h * z.so.head;
+  unsigned char* const dst = static_cast<unsigned char*>(z->out) + slot.b * z->so.batch + slot.h * z->so.head;
 #pragma unroll
   for (int it = 0; it < 32 * D / 8 / 64; ++it) {
     const int id = it * 64 + lane, rr = id / (D / 8), ch = (id % (D / 8)) * 8, row = row0 + 32 * wave + rr;
-    if (row >= z.w.Lq) continue;
+    if (row >= z->w.Lq) continue;
     const float4 val[2] = {*reinterpret_cast<const float4*>(other + rr * OSTRIDE + ch), *reinterpret_cast<const float4*>(other + rr * OSTRIDE + ch + 4)};
-    if (parts) store8<true>(z.part_o + (blockIdx.y * rows + id0 + row) * D + ch, val, 0);
-    else store8<false>(dst + row * z.so.token + ch * 2, val, 0);
+    if (parts) store8<true>(z->part_o + (blockIdx.y * rows + id0 + row) * D + ch, val, 0);
+    else store8<false>(dst + row * z->so.token + ch * 2, val, 0);
   }
 }
 
@@ -447,7 +467,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
 hipError_t launch_window_bf16(const WindowArgs& a, int d, hipStream_t st) {
   const dim3 grid((unsigned)((a.w.Lq + kWindowRows - 1) / kWindowRows * a.w.B * a.w.Hq), a.splits);
   if (d == 128) window_fwd_bf16<128, 2, 4><<<grid, 64 * NW, 0, st>>>(a);
-  else window_fwd_bf16<64, 3, 2><<<grid, 64 * NW, 0, st>>>(a);
+  else window_fwd_bf16<64, 3, 4><<<grid, 64 * NW, 0, st>>>(a);
   return hipGetLastError();
 }
 
