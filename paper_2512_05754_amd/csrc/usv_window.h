@@ -33,6 +33,7 @@ struct WindowArgs {
   float scale;
   int splits;  // > 1: the key list is shared out, results go to part_o [splits][rows][d] (normalised, fp32) and part_lse [splits][rows]
   float *part_o, *part_lse;
+  int period;  // bf16 kernel: see there
 };
 
 struct WindowGradArgs {

@@ -28,6 +28,8 @@ namespace {
 constexpr int NW = 2;
 constexpr int kItem = 4096;
 constexpr int kStep = 32;                // entries of a wave's step
+template <int D>
+constexpr int kTogether = D == 128 ? 128 : 192;  // workgroups that an XCD runs together
 constexpr float kNoKey = 3.4028234e38f;  // reference of a row that has seen no key yet
 
 // One item, global -> LDS: instruction r takes rows 8 r .. 8 r + 7 and lands at lds + 1024 r + 16 * lane.  Its offset field is added to the
@@ -71,7 +73,7 @@ __device__ __forceinline__ ArgsAgain again() {
 
 // QL: Q fragments of the last channel step that are read back from LDS, four more reads a step.  All of Q in registers is 1 to 2 % faster where
 // every step is hot, but the other steps then spill: 480p frames, left 6, 1.94 ms against 2.05 (QL = 2: 1.99); d = 64, window 1000, 97.3 against 102.9 us.
-template <int D, int WPS, int QL>
+template <int D, int WPS, int QL, bool CIRCLE>
 __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   constexpr int KS = D / 32, DT = D / 16, OT = (DT + 3) / 4;
   constexpr int LINES = D / 64, IPS = 2 * LINES;
@@ -96,11 +98,39 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // Entries of this workgroup: tiles of 64 that end where the list does; what is missing from a whole number of them is missing ahead of
-  // entry 0, in the tile that is waited for anyway.  This wave's steps are at first + 64 n.
+  // entry 0.  This wave's half of tile t begins at entry entry_of(t).
+  // CIRCLE: workgroups that run together have windows that lie one behind the other.  Each begun at its own first key, they read a key at
+  // different times, and the L2 has lost it in between.  So the window's tiles are walked in a circle, from the first key that is a multiple of
+  // `period`, the length of a window, to the end and on from the beginning: begun at one time, all read the same keys at the same time, and go on
+  // doing so in the next round.  Two things take them apart: the waves of a SIMD, which therefore take turns (s_setprio by step and slot),
+  // and the rounds, whose starts spread by about 0.3 sqrt(round) of a sweep; a workgroup begins as much further on as its place in the round is
+  // expected to be late.  (720p frames, left and right 3: 15.4 ms; circle 15.1, with turns 14.3, starts spread by 0.2 / 0.3 / 0.5
+  // sqrt(round) 12.4 / 11.7 / 11.8.)
   const int tiles = (keys.count + 63) / 64;
   const int t0 = __builtin_amdgcn_readfirstlane((int)((long long)tiles * blockIdx.y / a.splits));
   const int n_steps = __builtin_amdgcn_readfirstlane((int)((long long)tiles * (blockIdx.y + 1) / a.splits)) - t0;
-  const int first = keys.count - (tiles - t0) * 64 + wave * kStep;
+  const int start = keys.count - tiles * 64;  // of tile 0
+  const int head_tiles = keys.head > 0 ? (keys.head - start + 63) / 64 : 0;
+  int turn = 0;  // tiles between the window's first and the one that the circle begins with
+  if (CIRCLE && tiles > head_tiles) {
+    const int lo = keys.head + keys.skip, key = (lo + a.period - 1) / a.period * a.period;
+    if (key < keys.count + keys.skip) turn = max(0, (key - keys.skip - start) / 64 - head_tiles);
+    const int rank = blockIdx.x / kNumXcd, round = rank / kTogether<D>;
+    const float at = fminf(1.f, 0.3f * __builtin_amdgcn_sqrtf((float)round)) * ((float)(rank - round * kTogether<D>) * (1.f / kTogether<D>) - 0.5f);
+    const int n = tiles - head_tiles;
+    turn += (int)(at * (float)n);
+    turn = turn < 0 ? turn + n : turn >= n ? turn - n : turn;
+    turn = __builtin_amdgcn_readfirstlane(turn);
+  }
+  auto tile_of = [&](int n) {
+    int t = t0 + n;
+    if (t >= head_tiles) {
+      t += turn;
+      if (t >= tiles) t -= tiles - head_tiles;
+    }
+    return t;
+  };
+  auto entry_of = [&](int t) { return start + 64 * t + wave * kStep; };
 
   if (threadIdx.x < kWindowRows) {
     const int row = row0 + threadIdx.x;
@@ -144,22 +174,22 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
     const ArgsAgain b = again();
     const unsigned long long kb0 = reinterpret_cast<unsigned long long>(b->k) + slot.b * b->sk.batch + hk * b->sk.head;
     const unsigned long long vb0 = reinterpret_cast<unsigned long long>(b->v) + slot.b * b->sv.batch + hk * b->sv.head;
-#pragma unroll 1
-    for (int r = 0; r < 4; ++r) {
-      const long long key = window_key(keys, max(e + 8 * r + (ln >> 3), 0));
-      const unsigned kc = ((ln & 7) ^ (((4 * r) & 7) ^ (ln >> 4))) << 4, vc = ((ln & 7) ^ (((ln >> 4) & 3) << 1)) << 4;
+    // (item by item, as the waits count them)
 #pragma unroll
-      for (int line = 0; line < LINES; ++line) {
-        dma_lane(wave_lds + line * kItem + 1024 * r, kb0 + key * b->sk.token + line * 128 + kc);
-        dma_lane(wave_lds + (LINES + line) * kItem + 1024 * r, vb0 + key * b->sv.token + line * 128 + vc);
+    for (int x = 0; x < IPS; ++x)
+#pragma unroll 1
+      for (int r = 0; r < 4; ++r) {
+        const long long key = window_key(keys, max(e + 8 * r + (ln >> 3), 0));
+        const unsigned kc = ((ln & 7) ^ (((4 * r) & 7) ^ (ln >> 4))) << 4, vc = ((ln & 7) ^ (((ln >> 4) & 3) << 1)) << 4;
+        dma_lane(wave_lds + x * kItem + 1024 * r, (x < LINES ? kb0 + key * b->sk.token + kc : vb0 + key * b->sv.token + vc) + x % LINES * 128);
       }
-    }
   };
   using I0 = std::integral_constant<int, 0>;
   using I1 = std::integral_constant<int, 1>;
   using I2 = std::integral_constant<int, 2>;
   using I3 = std::integral_constant<int, 3>;
   if (n_steps > 0) {
+    const int first = entry_of(tile_of(0));
     point_at(first);
     if (plain_step(first)) {
       dma(I0{});
@@ -220,7 +250,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   // its rows need addresses of their own.
   auto step = [&](auto hot_c, int n) {
     constexpr bool HOT = decltype(hot_c)::value;
-    const int e0 = first + 64 * n, e1 = e0 + 64;
+    const int e0 = HOT ? 0 : entry_of(tile_of(n)), e1 = HOT ? 0 : entry_of(tile_of(n + 1));
     const bool more = HOT || n + 1 < n_steps, ahead = HOT || (more && plain_step(e1));
     if constexpr (HOT) {
 #pragma unroll
@@ -369,16 +399,32 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   };
   // hot steps in a row from step n on
   auto hot_steps = [&](int n) {
-    const int e0 = first + 64 * n, key = window_key(keys, e0);
+    const int t = tile_of(n), e0 = entry_of(t), key = window_key(keys, e0);
     if (e0 < 0 || (key < keys.all_lo && key >= keys.all_sink)) return 0;
     const int open = e0 < keys.head || key < keys.all_lo ? keys.all_sink : keys.all_hi;  // (keys below are seen by every row)
-    int k = min(n_steps - 1 - n, (open - key + kStep) / 64);                               // the step's keys lie below
+    int k = min(n_steps - 1 - n, (open - key + kStep) / 64);  // the step's keys lie below
+    k = min(k, (t < head_tiles ? head_tiles : tiles) - 1 - t);  // the next tile is the one behind it
     if (e0 < keys.head) k = min(k, (keys.head - e0 - kStep) / 64);                         // the next step's too
     return max(k, 0);
   };
+  unsigned pace = CIRCLE ? __builtin_amdgcn_s_getreg(4 | (3 << 11)) : 0;  // HW_ID, bits 0..3: the wave's slot of its SIMD
+  if (WPS == 3) pace %= 3;
+  auto next_turn = [&]() {
+    if constexpr (CIRCLE) {
+      if (WPS == 2 ? pace & 1 : pace == 1) __builtin_amdgcn_s_setprio(1);
+      else if (WPS == 3 && pace == 2) __builtin_amdgcn_s_setprio(2);
+      else __builtin_amdgcn_s_setprio(0);
+      ++pace;
+      if (WPS == 3 && pace == 3) pace = 0;
+    }
+  };
   for (int n = 0; n < n_steps;) {
     const int until = n + __builtin_amdgcn_readfirstlane(hot_steps(n));
-    for (; n < until; ++n) step(std::true_type{}, n);
+    for (; n < until; ++n) {
+      next_turn();
+      step(std::true_type{}, n);
+    }
+    next_turn();
     step(std::false_type{}, n);
     ++n;
   }
@@ -464,10 +510,26 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
 
 }  // namespace
 
-hipError_t launch_window_bf16(const WindowArgs& a, int d, hipStream_t st) {
-  const dim3 grid((unsigned)((a.w.Lq + kWindowRows - 1) / kWindowRows * a.w.B * a.w.Hq), a.splits);
-  if (d == 128) window_fwd_bf16<128, 2, 4><<<grid, 64 * NW, 0, st>>>(a);
-  else window_fwd_bf16<64, 3, 4><<<grid, 64 * NW, 0, st>>>(a);
+hipError_t launch_window_bf16(const WindowArgs& args, int d, hipStream_t st) {
+  const dim3 grid((unsigned)((args.w.Lq + kWindowRows - 1) / kWindowRows * args.w.B * args.w.Hq), args.splits);
+  WindowArgs a = args;
+  a.period = 0;
+  // Circles (CIRCLE) for windows with an end on both sides, from 1 MiB of K and V on.  In the order of the keys / in a circle, 12 heads, d = 128:
+  // 32768 tokens, left 4095 803 / 743 us, 8191 1429 / 1313; 480p frames, left 6 1899 / 1901, left 9 2371 / 2351, left and right 7 4027 / 3590; 3 heads,
+  // left 9 715 / 686; 720p frames, left and right 3 15.3 / 11.6 ms (L2 hits 44 % of its requests in the order of the keys, and the misses
+  // run at the fabric's 7 TB/s); four heads to a key head, 8000 tokens, left 4095 642 / 650; d = 64: left 1000 (0.3 MiB) 97.4 / 99.5, 16383 1315 / 1315.
+  // Without an end on either side all sweeps are the same and stay together better as they come: 32768 x 12 5686 / 5782, 75600 x 4 10642 / 12030.
+  if (a.splits == 1 && a.w.left >= 0 && a.w.right >= 0) {
+    const long long n = ((long long)a.w.left + a.w.right + 1 + (kWindowRows - 1) / a.w.chunk) * a.w.chunk;  // keys of a window
+    if (n < a.w.Lk && 4 * d * n >= (1 << 20)) a.period = (int)n;
+  }
+  auto launch = [&](auto circle) {
+    constexpr bool C = decltype(circle)::value;
+    if (d == 128) window_fwd_bf16<128, 2, 4, C><<<grid, 64 * NW, 0, st>>>(a);
+    else window_fwd_bf16<64, 3, 4, C><<<grid, 64 * NW, 0, st>>>(a);
+  };
+  if (a.period > 0) launch(std::true_type{});
+  else launch(std::false_type{});
   return hipGetLastError();
 }
 

@@ -160,6 +160,46 @@ def test_strides(usv, d, dtype):
         assert torch.equal(x, y) and bool((b[..., d:] == 7).all())
 
 
+def torch_rows(q, k, v, M, scale):
+    """out, lse and sum P |v| of one head in 64 bits on the GPU: q [Lq, d], k, v [Lk, d], M [Lq, Lk]."""
+    x = (q.double() @ k.double().T * scale).masked_fill(~M, -float("inf"))
+    lse = torch.logsumexp(x, 1)
+    P = torch.exp(x - lse[:, None])
+    return P @ v.double(), lse, P @ v.double().abs()
+
+
+@pytest.mark.parametrize("d, left, right, sinks, chunk", [(128, 2200, 0, 70, 1), (128, 3, 2, 1, 517), (64, 4200, 0, 3, 1), (64, 5, 1, 0, 700)])
+def test_long_windows_of_many_rows(usv, d, left, right, sinks, chunk):
+    """Launches of more than a round of workgroups with windows of more than a MiB: the keys are walked in a circle."""
+    H, L = 17, 6400
+    q, k, v = (normal((1, H, L, d), 200 + i, torch.bfloat16).to(DEV) for i in range(3))
+    out, lse = usv.window_attn(q, k, v, left, right, sinks, chunk, return_lse=True)
+    M = torch.from_numpy(wo.masks(1, L, L, left, right, sinks, chunk)[0]).to(DEV)
+    for h in (0, 3, 7, 16):
+        ref, ls, mag = torch_rows(q[0, h], k[0, h], v[0, h], M, d ** -0.5)
+        close(out[0, h], f64(ref), f64(mag), "bf16", f"head {h}")
+        close_lse(lse[0, h], f64(ls))
+    again = usv.window_attn(q, k, v, left, right, sinks, chunk, return_lse=True)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_long_windows_of_few_rows(usv, d):
+    """In one piece and shared out, from one row to a block and a bit, the first key of the list at any place of a tile."""
+    L, left = 5000, 4300
+    k, v = (normal((1, 1, L, d), 210 + i, torch.bfloat16).to(DEV) for i in range(2))
+    for n in (1, 63, 65, 130):
+        q = normal((1, 2, n, d), 220 + n, torch.bfloat16).to(DEV)
+        for sinks in (0, 1, 64, 200):
+            M = torch.from_numpy(wo.masks(1, n, L, left, 0, sinks, 1)[0]).to(DEV)
+            for ws in (None, torch.empty(0, dtype=torch.uint8, device=DEV)):
+                out, lse = usv.window_attn(q, k, v, left, 0, sinks, workspace=ws, return_lse=True)
+                for h in range(2):
+                    ref, ls, mag = torch_rows(q[0, h], k[0, 0], v[0, 0], M, d ** -0.5)
+                    close(out[0, h], f64(ref), f64(mag), "bf16", f"{n} rows, {sinks} sinks")
+                    close_lse(lse[0, h], f64(ls))
+
+
 def test_empty_lengths(usv):
     q, k = torch.zeros((1, 2, 0, 64), device=DEV), torch.randn((1, 2, 5, 64), device=DEV)
     out, lse = usv.window_attn(q, k, k, -1, return_lse=True)
