@@ -614,7 +614,7 @@ typedef struct {
 /* Bytes of the buffer (page_table and batch are not used).  0 for an invalid `c`. */
 size_t usv_cache_bytes(const usv_cache* c);
 
-/* Writes row i < rows of sequence b to position starts[b] + i.
+/* Writes row i < rows (at most 2^26) of sequence b to position starts[b] + i.
  * k, v   : [batch, kv_heads, rows, d] of dtype (device, read only), element strides k_strides, v_strides (NULL =
  *          contiguous; as those of usv_window)
  * starts : device int32 [batch];  counts : NULL, or device int32 [batch]: only rows i < counts[b] are written

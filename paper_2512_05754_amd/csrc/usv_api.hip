@@ -157,7 +157,7 @@ usv_status check_window(const usv_window* w, usv::WindowShape* s) {
     return fail(USV_ERR_INVALID_ARG, "q_start (%d) must be in [-2^30, 2^30] or USV_Q_AT_END", w->q_start);
   const long long heads = (long long)w->batch * w->q_heads;
   if (heads > 65535) return fail(USV_ERR_UNSUPPORTED, "batch * q_heads must be <= 65535");
-  if (heads * ((w->q_len > w->kv_len ? w->q_len : w->kv_len) / usv::kWindowRows + 1) > 0x7fffffffLL / 64)
+  if (heads * ((w->q_len > w->kv_len ? w->q_len : w->kv_len) / usv::kWindowRows + 1) > 0x7fffffffLL / 256)
     return fail(USV_ERR_UNSUPPORTED, "batch * q_heads * length too large");
   s->B = w->batch, s->Hq = w->q_heads, s->Hkv = w->kv_heads, s->group = w->q_heads / w->kv_heads;
   s->Lq = w->q_len, s->Lk = w->kv_len;
@@ -167,6 +167,7 @@ usv_status check_window(const usv_window* w, usv::WindowShape* s) {
   s->at_end = w->q_start == USV_Q_AT_END;
   s->q_start = s->at_end ? 0 : w->q_start;
   s->lens = w->seq_lens;
+  usv::window_divs(s);
   if (reinterpret_cast<uintptr_t>(w->seq_lens) & 3u) return fail(USV_ERR_INVALID_ARG, "seq_lens is not 4-byte aligned");
   return USV_OK;
 }
@@ -218,6 +219,7 @@ void window_grad_plan(usv::WindowGradArgs* g, int block, int rows_per_tile, int 
   auto parts = [&](long long list) { return list > 2 * piece ? (int)((list + piece - 1) / piece) : 1; };
   g->sink_parts = parts(sink_list);
   g->parts = parts(longest);
+  g->by_heads = usv::div_by((unsigned)heads), g->by_sink_parts = usv::div_by(g->sink_parts), g->by_parts = usv::div_by(g->parts);
 }
 size_t window_delta_bytes(const usv::WindowShape& s, bool bf16) { return ((size_t)s.B * s.Hq * s.Lq * (bf16 ? 16 : 4) + 255) / 256 * 256; }
 size_t window_partial_bytes(const usv::WindowGradArgs& g, int d) {
@@ -241,7 +243,7 @@ usv_status check_cache(const usv_cache* c, usv::CacheShape* s) {
   if (c->pages < 1) return fail(USV_ERR_INVALID_ARG, "pages must be >= 1");
   if (c->table_pages < 1 || (long long)c->table_pages * c->page_size > kMostTokens)
     return fail(USV_ERR_INVALID_ARG, "table_pages (%d) must be >= 1 and cover at most 2^30 positions", c->table_pages);
-  *s = usv::CacheShape{c->batch, c->kv_heads, c->head_dim, c->bits, c->page_size, c->pages, c->table_pages, c->page_table};
+  *s = usv::CacheShape{c->batch, c->kv_heads, c->head_dim, c->bits, c->page_size, c->pages, c->table_pages, c->page_table, usv::div_by(c->page_size), usv::div_by(c->page_size / usv::kCacheGroup)};
   return USV_OK;
 }
 
@@ -250,8 +252,7 @@ usv_status check_cache_rows(const void* cache, const usv_cache* c, const void* k
   const usv_status st = check_cache(c, &a->c);
   if (st != USV_OK) return st;
   if (dtype != USV_F32 && dtype != USV_BF16) return fail(USV_ERR_UNSUPPORTED, "dtype must be USV_F32 or USV_BF16 (got %d)", dtype);
-  if (rows < 0 || rows > kMostTokens || (long long)rows * c->batch * c->kv_heads > (1LL << 34))
-    return fail(USV_ERR_INVALID_ARG, "rows (%d) must be in [0, 2^30] and batch * kv_heads * rows at most 2^34", rows);
+  if (rows < 0 || rows > (1 << 26)) return fail(USV_ERR_INVALID_ARG, "rows (%d) must be in [0, 2^26]", rows);
   const usv_strides none = {0, 0, 0};
   const long long esz = dtype == USV_BF16 ? 2 : 4;
   usv_status bad = check_window_strides("k", ks ? *ks : none, c->kv_heads, rows, c->head_dim, esz, written, &a->sk);

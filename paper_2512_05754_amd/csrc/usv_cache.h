@@ -12,6 +12,7 @@ namespace usv {
 struct CacheShape {
   int B, H, d, bits, page_size, pages, table_pages;
   const int32_t* table;  // [B, table_pages]
+  Div by_page, by_groups;  // page_size; page_size / 16
   __host__ __device__ int code_bytes() const { return d * bits / 8; }
   __host__ __device__ int scale_bytes() const { return d / 32; }
   __host__ __device__ long long head_bytes() const { return 2LL * page_size * (code_bytes() + scale_bytes()); }
@@ -30,7 +31,6 @@ struct CacheAttnArgs {
   CacheShape c;
   const unsigned char* cache;
   WindowArgs f;  // q, out, lse, pieces; k, v unused
-  unsigned div_mul, div_shift;  // x / (page_size / 16) = (mulhi(x, div_mul) + x) >> div_shift, x < 2^27
 };
 
 constexpr int kCacheGroup = 16;  // keys of a page that are looked up together; page_size is a multiple

@@ -47,16 +47,14 @@ struct Place {
 template <int D>
 __device__ __forceinline__ bool place_of(const CacheRowsArgs& a, Place* p) {
   constexpr int PER = D / 8;
-  const long long id = (long long)blockIdx.x * (256 / PER) + threadIdx.x / PER;
-  if (id >= (long long)a.c.B * a.c.H * a.rows) return false;
-  p->i = (int)(id % a.rows);
-  const int bh = (int)(id / a.rows);
-  p->b = bh / a.c.H, p->h = bh % a.c.H;
+  const long long i = (long long)blockIdx.x * (256 / PER) + threadIdx.x / PER;
+  if (i >= a.rows) return false;
+  p->i = (int)i, p->h = blockIdx.y, p->b = blockIdx.z;
   if (a.counts && p->i >= a.counts[p->b]) return false;
   const long long pos = (long long)a.starts[p->b] + p->i;
   p->page = -1, p->row = 0;
   if (pos >= 0 && pos < (long long)a.c.table_pages * a.c.page_size) {
-    const int slot = (int)(pos / a.c.page_size);
+    const int slot = (int)pos / a.c.by_page;
     p->row = (int)(pos - (long long)slot * a.c.page_size);
     const int page = a.c.table[(long long)p->b * a.c.table_pages + slot];
     if (page >= 0 && page < a.c.pages) p->page = page;
@@ -156,8 +154,8 @@ __global__ __launch_bounds__(256) void cache_read(CacheRowsArgs a) {
 
 template <typename F>
 hipError_t by_kind(const CacheRowsArgs& a, bool bf16, F f) {
-  const long long rows = (long long)a.c.B * a.c.H * a.rows, per = 256 / (a.c.d / 8);
-  const unsigned grid = (unsigned)((rows + per - 1) / per);
+  const int per = 256 / (a.c.d / 8);
+  const dim3 grid((a.rows + per - 1) / per, a.c.H, a.c.B);
   auto with = [&](auto t, auto d) {
     if (a.c.bits == 4) f(t, d, std::integral_constant<int, 4>{}, grid);
     else f(t, d, std::integral_constant<int, 8>{}, grid);
@@ -174,12 +172,12 @@ hipError_t by_kind(const CacheRowsArgs& a, bool bf16, F f) {
 }  // namespace
 
 hipError_t launch_cache_write(const CacheRowsArgs& a, bool bf16, hipStream_t st) {
-  return by_kind(a, bf16, [&](auto t, auto d, auto bits, unsigned grid) {
+  return by_kind(a, bf16, [&](auto t, auto d, auto bits, const dim3& grid) {
     cache_write<decltype(t), decltype(d)::value, decltype(bits)::value><<<grid, 256, 0, st>>>(a);
   });
 }
 hipError_t launch_cache_read(const CacheRowsArgs& a, bool bf16, hipStream_t st) {
-  return by_kind(a, bf16, [&](auto t, auto d, auto bits, unsigned grid) {
+  return by_kind(a, bf16, [&](auto t, auto d, auto bits, const dim3& grid) {
     cache_read<decltype(t), decltype(d)::value, decltype(bits)::value><<<grid, 256, 0, st>>>(a);
   });
 }

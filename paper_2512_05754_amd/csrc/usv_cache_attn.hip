@@ -80,7 +80,7 @@ __device__ __forceinline__ const unsigned char* uniform(const unsigned char* p) 
 }
 
 template <int D, int BITS, int NT>
-__global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void cache_attn(CacheAttnArgs a, int row_tiles) {
+__global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void cache_attn(CacheAttnArgs a, Div by_tiles) {
   constexpr int ROWS = 16 * NT, KS = D / 32, DT = D / 16, OT = DT / 4, CB = D * BITS / 8, SB = D / 32;
   constexpr int PITCH = D * 2 + 16, AREA = 32 * PITCH, OPITCH = D + 4;
   constexpr bool QLDS = NT == 4;  // there are no registers for 64 rows of Q: read back from LDS, each fragment for two products
@@ -92,10 +92,10 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void cache_attn(CacheAttnArgs
   const WindowShape& w = a.f.w;
   const int lane = threadIdx.x & 63, c = lane & 15, G = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int tile = blockIdx.x % row_tiles, bh = blockIdx.x / row_tiles, b = bh / w.Hkv, hk = bh % w.Hkv;
+  const int bh = (int)blockIdx.x / by_tiles, tile = (int)blockIdx.x - bh * (int)by_tiles.n, b = bh / w.by_hkv, hk = bh - b * w.Hkv;
   const WindowSeq seq = window_seq_of(w, b);
   const int all_rows = w.Lq * w.group, row0 = tile * ROWS, row1 = min(row0 + ROWS, all_rows);
-  const int i0 = row0 / w.group, i1 = (row1 - 1) / w.group + 1;  // query tokens
+  const int i0 = row0 / w.by_group, i1 = (row1 - 1) / w.by_group + 1;  // query tokens
   WindowKeys keys = window_keys(w, seq, i0, i1 - i0);
   window_uniform(&keys);
   // groups of 16 keys: list entry x is group x where x < head_groups, else x + skip_groups
@@ -104,13 +104,14 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void cache_attn(CacheAttnArgs
   const int skip_groups = max(0, lo / kCacheGroup - head_groups);
   const int groups = keys.count > 0 ? (hi + kCacheGroup - 1) / kCacheGroup - skip_groups : 0;
   const int steps = (groups + 1) / 2;
-  const int s0 = __builtin_amdgcn_readfirstlane((int)((long long)steps * blockIdx.y / a.f.splits));
-  const int s1 = __builtin_amdgcn_readfirstlane((int)((long long)steps * (blockIdx.y + 1) / a.f.splits));
+  int s0 = 0, s1 = steps;
+  if (a.f.splits > 1) s0 = (int)((long long)steps * blockIdx.y / a.f.splits), s1 = (int)((long long)steps * (blockIdx.y + 1) / a.f.splits);
+  s0 = __builtin_amdgcn_readfirstlane(s0), s1 = __builtin_amdgcn_readfirstlane(s1);
 
   const int32_t* const table = a.c.table + (long long)b * a.c.table_pages;
   unsigned char* const area = smem + wave * AREA;
   auto group_of = [&](int x) { return x < head_groups ? x : x + skip_groups; };
-  auto slot_of = [&](unsigned g) { return (__umulhi(g, a.div_mul) + g) >> a.div_shift; };
+  auto slot_of = [&](int g) { return g / a.c.by_groups; };
   // Pages of this wave's next 32 steps: lane 2 k + m holds that of group m of step first + 4 k.
   int pages_v = 0;
   auto look_up = [&](int first) {
@@ -121,12 +122,12 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void cache_attn(CacheAttnArgs
   if (step0 < s1) look_up(step0);
 
   for (int r = threadIdx.x; r < ROWS; r += 256) {
-    const WindowRange x = row0 + r < row1 ? window_range(w, seq.n, seq.first + (row0 + r) / w.group) : WindowRange{0, 0};
+    const WindowRange x = row0 + r < row1 ? window_range(w, seq.n, seq.first + (row0 + r) / w.by_group) : WindowRange{0, 0};
     srange[r] = make_int2(x.lo, x.hi);
   }
   // Q fragments: lane (c, G) has row 16 nt + c, channels D / 4 * G + 8 t .. + 8
   auto load_q = [&](int nt, int t) {
-    const int row = min(row0 + 16 * nt + c, row1 - 1), i = row / w.group, h = hk * w.group + row % w.group;
+    const int row = min(row0 + 16 * nt + c, row1 - 1), i = row / w.by_group, h = hk * w.group + row - i * w.group;
     const unsigned char* p = static_cast<const unsigned char*>(a.f.q) + b * a.f.sq.batch + h * a.f.sq.head + i * a.f.sq.token;
     return *reinterpret_cast<const bf16x8*>(p + (D / 4 * G + 8 * t) * 2);
   };
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void cache_attn(CacheAttnArgs
     for (int m = 0; m < 2; ++m) {
       const int g = __builtin_amdgcn_readfirstlane(group_of(min(2 * step + m, groups - 1)));
       const int page = __builtin_amdgcn_readlane(pages_v, 2 * k + m);
-      const int first = __builtin_amdgcn_readfirstlane((g - (int)slot_of(g) * page_groups) * kCacheGroup);
+      const int first = __builtin_amdgcn_readfirstlane((g - slot_of(g) * page_groups) * kCacheGroup);
       const unsigned char* base = uniform(a.cache + ((unsigned long long)page * w.Hkv + hk) * head_bytes);
       int row = c;
       const int j0 = g * kCacheGroup;
@@ -311,7 +312,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void cache_attn(CacheAttnArgs
     constexpr int CH = D / 16;
     const int r = threadIdx.x >> 4, ch = CH * (threadIdx.x & 15), row = row0 + 16 * nt + r;
     if (row < row1) {
-      const int i = row / w.group, h = hk * w.group + row % w.group;
+      const int i = row / w.by_group, h = hk * w.group + row - i * w.group;
       const long long id = ((long long)b * w.Hq + h) * w.Lq + i;
       const int2 range = srange[16 * nt + r];
       const bool live = range.y > 0;
@@ -344,19 +345,14 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void cache_attn(CacheAttnArgs
 
 }  // namespace
 
-hipError_t launch_cache_attn(const CacheAttnArgs& args, hipStream_t st) {
-  const WindowShape& w = args.f.w;
-  CacheAttnArgs a = args;
-  const unsigned n = a.c.page_size / kCacheGroup;
-  a.div_shift = 0;
-  while ((1u << a.div_shift) < n) ++a.div_shift;
-  a.div_mul = (unsigned)(((1ull << 32) * ((1ull << a.div_shift) - n)) / n + 1);
+hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t st) {
+  const WindowShape& w = a.f.w;
   const int rows = cache_attn_rows(w), tiles = (w.Lq * w.group + rows - 1) / rows;
   const dim3 grid((unsigned)(tiles * w.B * w.Hkv), a.f.splits);
   auto go = [&](auto d, auto bits) {
     constexpr int D = decltype(d)::value, BITS = decltype(bits)::value;
-    if (rows == 16) cache_attn<D, BITS, 1><<<grid, 256, 0, st>>>(a, tiles);
-    else cache_attn<D, BITS, 4><<<grid, 256, 0, st>>>(a, tiles);
+    if (rows == 16) cache_attn<D, BITS, 1><<<grid, 256, 0, st>>>(a, div_by(tiles));
+    else cache_attn<D, BITS, 4><<<grid, 256, 0, st>>>(a, div_by(tiles));
   };
   using D128 = std::integral_constant<int, 128>;
   using D64 = std::integral_constant<int, 64>;

@@ -12,6 +12,20 @@
 
 namespace usv {
 
+// Division by a number that the launch knows: x / n = (mulhi(x, mul) + x) >> shift, x < 2^31 (the round-up method; 3 instructions, where a
+// division takes 30, and one of 64 bits 150 on the way to a workgroup's first load).
+struct Div {
+  unsigned n, mul, shift;
+};
+inline Div div_by(unsigned n) {
+  Div d = {n ? n : 1, 0, 0};
+  while ((1ull << d.shift) < d.n) ++d.shift;
+  d.mul = (unsigned)(((1ull << 32) * ((1ull << d.shift) - d.n)) / d.n + 1);
+  return d;
+}
+__host__ __device__ inline int operator/(int x, const Div& d) { return (int)(((unsigned)(((unsigned long long)(unsigned)x * d.mul) >> 32) + (unsigned)x) >> d.shift); }
+__host__ __device__ inline int operator%(int x, const Div& d) { return x - x / d * (int)d.n; }
+
 struct Strides3 {
   long long batch, head, token;  // bytes
 };
@@ -22,7 +36,9 @@ struct WindowShape {
   int left, right, chunk, sink;  // sink in tokens; 0 where there is no left limit (nothing to add then)
   int q_start, at_end;           // position of query row 0; at_end: the last row is the sequence's last token
   const int32_t* lens;           // NULL, or [B] tokens of each sequence
+  Div by_chunk, by_group, by_hkv;
 };
+inline void window_divs(WindowShape* w) { w->by_chunk = div_by(w->chunk), w->by_group = div_by(w->group), w->by_hkv = div_by(w->Hkv); }
 
 struct WindowArgs {
   WindowShape w;
@@ -34,7 +50,12 @@ struct WindowArgs {
   int splits;  // > 1: the key list is shared out, results go to part_o [splits][rows][d] (normalised, fp32) and part_lse [splits][rows]
   float *part_o, *part_lse;
   int period;  // bf16 kernel: see there
+  Div by_items, by_rest, by_period;  // window_slot; period
 };
+// What window_slot needs for blocks of `rows` query rows.
+inline void window_slots(WindowArgs* a, int rows) {
+  a->by_items = div_by((a->w.Lq + rows - 1) / rows * a->w.group), a->by_rest = div_by(a->w.B * a->w.Hkv % kNumXcd);
+}
 
 struct WindowGradArgs {
   WindowArgs f;  // q, k, v, out, lse as the forward pass left them
@@ -45,6 +66,7 @@ struct WindowGradArgs {
   // Key blocks are `block` keys.  Those below sink_blocks (every later row sees them) have sink_parts pieces, the others parts.
   int block, blocks, sink_blocks, sink_parts, parts;
   float* partial;  // dk, dv of the pieces: [slot][2][block][d]; a block in one piece has no slot
+  Div by_heads, by_sink_parts, by_parts;
 };
 
 struct WindowSeq {
@@ -63,7 +85,7 @@ struct WindowRange {
 };
 __host__ __device__ inline WindowRange window_range(const WindowShape& w, int n, int p) {
   if (p < 0 || p >= n) return {0, 0};
-  const int c = p / w.chunk;
+  const int c = p / w.by_chunk;
   const long long end = ((long long)c + w.right + 1) * w.chunk, begin = ((long long)c - w.left) * w.chunk;
   WindowRange r;
   r.hi = w.right < 0 || end > n ? n : (int)end;
@@ -119,8 +141,8 @@ __host__ __device__ inline WindowRows window_rows(const WindowShape& w, const Wi
   if (k0 >= s.n) return {0, 0};
   const long long k1 = (long long)k0 + block < s.n ? (long long)k0 + block : s.n;
   long long p0 = 0, p1 = s.n;
-  if (w.right >= 0) p0 = ((long long)k0 / w.chunk - w.right) * w.chunk;
-  if (w.left >= 0 && k0 >= w.sink) p1 = ((k1 - 1) / w.chunk + w.left + 1) * w.chunk;
+  if (w.right >= 0) p0 = ((long long)(k0 / w.by_chunk) - w.right) * w.chunk;
+  if (w.left >= 0 && k0 >= w.sink) p1 = ((long long)((int)(k1 - 1) / w.by_chunk) + w.left + 1) * w.chunk;
   if (p0 < 0) p0 = 0;
   if (p1 > s.n) p1 = s.n;
   long long i0 = p0 - s.first, i1 = p1 - s.first;
@@ -136,16 +158,19 @@ __host__ __device__ inline WindowRows window_rows(const WindowShape& w, const Wi
 struct WindowSlot {
   int blk, b, h;
 };
-__device__ __forceinline__ WindowSlot window_slot(const WindowShape& w, int slot, int blocks) {
+__device__ __forceinline__ WindowSlot window_slot(const WindowArgs& a, int slot, int blocks) {
+  const WindowShape& w = a.w;
   const int heads = w.B * w.Hkv, items = blocks * w.group, whole = heads / kNumXcd;
   int y = slot / kNumXcd, unit, item;
   if (y < whole * items) {
-    unit = y / items * kNumXcd + slot % kNumXcd, item = y % items;
+    const int q = y / a.by_items;
+    unit = q * kNumXcd + slot % kNumXcd, item = y - q * items;
   } else {
     const int z = slot - whole * items * kNumXcd, rest = heads % kNumXcd;
-    unit = whole * kNumXcd + z % rest, item = z / rest;
+    item = z / a.by_rest, unit = whole * kNumXcd + z - item * rest;
   }
-  return {blocks - 1 - item / w.group, unit / w.Hkv, unit % w.Hkv * w.group + item % w.group};
+  const int i = item / w.by_group, b = unit / w.by_hkv;
+  return {blocks - 1 - i, b, (unit - b * w.Hkv) * w.group + item - i * w.group};
 }
 
 // Gradient of the keys: launch slot -> (key block, piece of its list of rows, head).  Blocks that every row sees come first, in pieces of
@@ -166,14 +191,15 @@ __host__ __device__ inline unsigned window_pieces(const WindowGradArgs& g) {
 __device__ __forceinline__ WindowPiece window_piece(const WindowGradArgs& g, int slot) {
   const int heads = g.f.w.B * g.f.w.Hkv;
   WindowPiece p;
-  int y = slot / heads, bh = slot % heads;
+  int y = slot / g.by_heads, bh = slot - y * heads;
   if (heads % kNumXcd == 0) bh = (bh % kNumXcd) * (heads / kNumXcd) + bh / kNumXcd;
   const bool sink = y < g.sink_blocks * g.sink_parts;
   if (!sink) y -= g.sink_blocks * g.sink_parts;
   p.parts = sink ? g.sink_parts : g.parts;
-  p.block = (sink ? 0 : g.sink_blocks) + y / p.parts;
-  p.part = y % p.parts;
-  p.b = bh / g.f.w.Hkv, p.h = bh % g.f.w.Hkv;
+  const int q = sink ? y / g.by_sink_parts : y / g.by_parts;
+  p.block = (sink ? 0 : g.sink_blocks) + q;
+  p.part = y - q * p.parts;
+  p.b = bh / g.f.w.by_hkv, p.h = bh - p.b * g.f.w.Hkv;
   p.slot = p.parts > 1 ? window_piece_slot(g, bh, p.block, p.part) : -1;
   return p;
 }

@@ -88,7 +88,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   __shared__ __attribute__((aligned(16))) unsigned char q_tail[QL > 0 ? QL * 1024 : 16];
 
   const WindowShape& w = a.w;
-  WindowSlot slot = window_slot(w, blockIdx.x, (w.Lq + kWindowRows - 1) / kWindowRows);
+  WindowSlot slot = window_slot(a, blockIdx.x, (w.Lq + kWindowRows - 1) / kWindowRows);
   slot.blk = __builtin_amdgcn_readfirstlane(slot.blk), slot.b = __builtin_amdgcn_readfirstlane(slot.b), slot.h = __builtin_amdgcn_readfirstlane(slot.h);
   const WindowSeq seq = window_seq_of(w, slot.b);
   const int row0 = slot.blk * kWindowRows;
@@ -107,13 +107,15 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   // expected to be late.  (720p frames, left and right 3: 15.4 ms; circle 15.1, with turns 14.3, starts spread by 0.2 / 0.3 / 0.5
   // sqrt(round) 12.4 / 11.7 / 11.8.)
   const int tiles = (keys.count + 63) / 64;
-  const int t0 = __builtin_amdgcn_readfirstlane((int)((long long)tiles * blockIdx.y / a.splits));
-  const int n_steps = __builtin_amdgcn_readfirstlane((int)((long long)tiles * (blockIdx.y + 1) / a.splits)) - t0;
+  int t0 = 0, t1 = tiles;
+  if (a.splits > 1) t0 = (int)((long long)tiles * blockIdx.y / a.splits), t1 = (int)((long long)tiles * (blockIdx.y + 1) / a.splits);
+  t0 = __builtin_amdgcn_readfirstlane(t0);
+  const int n_steps = __builtin_amdgcn_readfirstlane(t1) - t0;
   const int start = keys.count - tiles * 64;  // of tile 0
   const int head_tiles = keys.head > 0 ? (keys.head - start + 63) / 64 : 0;
   int turn = 0;  // tiles between the window's first and the one that the circle begins with
   if (CIRCLE && tiles > head_tiles) {
-    const int lo = keys.head + keys.skip, key = (lo + a.period - 1) / a.period * a.period;
+    const int lo = keys.head + keys.skip, key = (lo + a.period - 1) / a.by_period * a.period;
     if (key < keys.count + keys.skip) turn = max(0, (key - keys.skip - start) / 64 - head_tiles);
     const int rank = blockIdx.x / kNumXcd, round = rank / kTogether<D>;
     const float at = fminf(1.f, 0.3f * __builtin_amdgcn_sqrtf((float)round)) * ((float)(rank - round * kTogether<D>) * (1.f / kTogether<D>) - 0.5f);
@@ -138,7 +140,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
     srange[threadIdx.x] = make_int2(r.lo, r.hi);
   }
 
-  const int hk = __builtin_amdgcn_readfirstlane(slot.h / w.group);
+  const int hk = __builtin_amdgcn_readfirstlane(slot.h / w.by_group);
   const unsigned wave_lds = lds_address(smem) + wave * kWaveBytes;
   // DMA lane -> row lane / 8 of an instruction's 8 rows, 16-byte chunk lane % 8 of the line; K chunks are stored at chunk ^ (row / 2 % 8), V
   // chunks at chunk ^ 2 (row / 2 % 4)
@@ -528,6 +530,8 @@ hipError_t launch_window_bf16(const WindowArgs& args, int d, hipStream_t st) {
     if (d == 128) window_fwd_bf16<128, 2, 4, C><<<grid, 64 * NW, 0, st>>>(a);
     else window_fwd_bf16<64, 3, 4, C><<<grid, 64 * NW, 0, st>>>(a);
   };
+  a.by_period = div_by(a.period);
+  window_slots(&a, kWindowRows);
   if (a.period > 0) launch(std::true_type{});
   else launch(std::false_type{});
   return hipGetLastError();

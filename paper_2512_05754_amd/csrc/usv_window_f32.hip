@@ -93,15 +93,16 @@ template <typename T, int D>
 __global__ __launch_bounds__(256) void window_fwd(WindowArgs a) {
   __shared__ __attribute__((aligned(16))) float sk[kTile * (D + 4)], sv[kTile * (D + 4)];
   const int blocks = (a.w.Lq + kWindowRows - 1) / kWindowRows;
-  const WindowSlot at_ = window_slot(a.w, blockIdx.x, blocks);
-  const int hk = at_.h / a.w.group;
+  const WindowSlot at_ = window_slot(a, blockIdx.x, blocks);
+  const int hk = at_.h / a.w.by_group;
   const WindowSeq seq = window_seq_of(a.w, at_.b);
   const WindowKeys keys = window_keys(a.w, seq, (long long)at_.blk * kWindowRows, kWindowRows);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, G = lane >> 4;
   const int row = at_.blk * kWindowRows + 16 * wave + c;
   const bool live = row >= keys.i0 && row < keys.i1;
   const int tiles = (keys.count + kTile - 1) / kTile;
-  const int t0 = (int)((long long)tiles * blockIdx.y / a.splits), t1 = (int)((long long)tiles * (blockIdx.y + 1) / a.splits);
+  int t0 = 0, t1 = tiles;
+  if (a.splits > 1) t0 = (int)((long long)tiles * blockIdx.y / a.splits), t1 = (int)((long long)tiles * (blockIdx.y + 1) / a.splits);
 
   f32x4 o[D / 16];
 #pragma unroll
@@ -232,8 +233,8 @@ __global__ __launch_bounds__(256) void window_grad_q(WindowGradArgs g) {
   const WindowArgs& a = g.f;
   __shared__ __attribute__((aligned(16))) float sk[kTile * (D + 4)], sv[kTile * (D + 4)];
   const int blocks = (a.w.Lq + kWindowRows - 1) / kWindowRows;
-  const WindowSlot at_ = window_slot(a.w, blockIdx.x, blocks);
-  const int hk = at_.h / a.w.group;
+  const WindowSlot at_ = window_slot(a, blockIdx.x, blocks);
+  const int hk = at_.h / a.w.by_group;
   const WindowSeq seq = window_seq_of(a.w, at_.b);
   const WindowKeys keys = window_keys(a.w, seq, (long long)at_.blk * kWindowRows, kWindowRows);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, G = lane >> 4;
@@ -314,7 +315,8 @@ __global__ __launch_bounds__(256) void window_grad_kv(WindowGradArgs g) {
   for (int dt = 0; dt < D / 16; ++dt) dk[dt] = dv[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int tiles = (rows.i1 - rows.i0 + kTile - 1) / kTile;
   const long long all = (long long)tiles * a.w.group;
-  const int n0 = (int)(all * pc.part / pc.parts), n1 = (int)(all * (pc.part + 1) / pc.parts);
+  int n0 = 0, n1 = (int)all;
+  if (pc.parts > 1) n0 = (int)(all * pc.part / pc.parts), n1 = (int)(all * (pc.part + 1) / pc.parts);
   if (n0 < n1) {
     const int krow = min(key, seq.n - 1);
     float4 kf[D / 16], vf[D / 16];
@@ -413,7 +415,9 @@ hipError_t by_type(bool bf16, int d, F f) {
 
 }  // namespace
 
-hipError_t launch_window_f32(const WindowArgs& a, int d, hipStream_t st) {
+hipError_t launch_window_f32(const WindowArgs& args, int d, hipStream_t st) {
+  WindowArgs a = args;
+  window_slots(&a, kWindowRows);
   const dim3 grid((unsigned)((a.w.Lq + kWindowRows - 1) / kWindowRows * a.w.B * a.w.Hq), a.splits);
   if (d == 128) window_fwd<float, 128><<<grid, 256, 0, st>>>(a);
   else window_fwd<float, 64><<<grid, 256, 0, st>>>(a);
@@ -428,7 +432,9 @@ hipError_t launch_window_join(const WindowArgs& a, bool bf16, int d, hipStream_t
   });
 }
 
-hipError_t launch_window_grad_f32(const WindowGradArgs& g, int d, hipStream_t st) {
+hipError_t launch_window_grad_f32(const WindowGradArgs& args, int d, hipStream_t st) {
+  WindowGradArgs g = args;
+  window_slots(&g.f, kWindowRows);
   const unsigned q_grid = (unsigned)((g.f.w.Lq + kWindowRows - 1) / kWindowRows * g.f.w.B * g.f.w.Hq);
   auto go = [&](auto dc) {
     constexpr int D = decltype(dc)::value;

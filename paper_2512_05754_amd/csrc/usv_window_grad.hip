@@ -163,8 +163,8 @@ __global__ __launch_bounds__(256, WPS) void window_grad_q_bf16(WindowGradArgs g)
   using T = Tile<D>;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * T::STAGE];
   const WindowArgs& a = g.f;
-  const WindowSlot slot = window_slot(a.w, blockIdx.x, (a.w.Lq + kBlock128 - 1) / kBlock128);
-  const int hk = slot.h / a.w.group;
+  const WindowSlot slot = window_slot(a, blockIdx.x, (a.w.Lq + kBlock128 - 1) / kBlock128);
+  const int hk = slot.h / a.w.by_group;
   const WindowSeq seq = window_seq_of(a.w, slot.b);
   WindowKeys keys = window_keys(a.w, seq, (long long)slot.blk * kBlock128, kBlock128);
   window_uniform(&keys);
@@ -284,7 +284,9 @@ __global__ __launch_bounds__(256, WPS) void window_grad_kv_bf16(WindowGradArgs g
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tiles = (i1 - i0 + kRows - 1) / kRows;
   const long long all = (long long)tiles * a.w.group;
-  const int n0 = __builtin_amdgcn_readfirstlane((int)(all * pc.part / pc.parts)), n1 = __builtin_amdgcn_readfirstlane((int)(all * (pc.part + 1) / pc.parts));
+  int n0 = 0, n1 = (int)all;
+  if (pc.parts > 1) n0 = (int)(all * pc.part / pc.parts), n1 = (int)(all * (pc.part + 1) / pc.parts);
+  n0 = __builtin_amdgcn_readfirstlane(n0), n1 = __builtin_amdgcn_readfirstlane(n1);
   f32x16 dk[2][D / 64], dv[2][D / 64];
   clear<D>(dk);
   clear<D>(dv);
@@ -294,8 +296,8 @@ __global__ __launch_bounds__(256, WPS) void window_grad_kv_bf16(WindowGradArgs g
     {
       const long long end = (long long)k0 + kBlock128;
       if (end > seq.n) o1 = o0;
-      if (a.w.right >= 0) o0 = (int)min((long long)i1, max((long long)i0, ((end + a.w.chunk - 1) / a.w.chunk - a.w.right - 1) * a.w.chunk - seq.first));
-      if (a.w.left >= 0 && end > a.w.sink) o1 = (int)min((long long)o1, max((long long)i0, ((long long)k0 / a.w.chunk + a.w.left + 1) * a.w.chunk - seq.first));
+      if (a.w.right >= 0) o0 = (int)min((long long)i1, max((long long)i0, ((long long)((int)(end - 1) / a.w.by_chunk) - a.w.right) * a.w.chunk - seq.first));
+      if (a.w.left >= 0 && end > a.w.sink) o1 = (int)min((long long)o1, max((long long)i0, ((long long)(k0 / a.w.by_chunk) + a.w.left + 1) * a.w.chunk - seq.first));
       o0 = __builtin_amdgcn_readfirstlane(o0), o1 = __builtin_amdgcn_readfirstlane(o1);
     }
     const unsigned lds = lds_address(smem), lds_row = lds_address(srow);
@@ -312,7 +314,8 @@ __global__ __launch_bounds__(256, WPS) void window_grad_kv_bf16(WindowGradArgs g
         dma_lane(lds_row + stage * (kRows * 16), reinterpret_cast<unsigned long long>(reinterpret_cast<const float4*>(g.delta) + id));
       }
     };
-    int h = pc.h * a.w.group + n0 / tiles, t = n0 % tiles;
+    int h = pc.h * a.w.group, t = n0;
+    if (n0 > 0) h += n0 / tiles, t = n0 % tiles;
     h = __builtin_amdgcn_readfirstlane(h), t = __builtin_amdgcn_readfirstlane(t);
     request(h, t, 0);
 
@@ -421,7 +424,9 @@ __global__ __launch_bounds__(256, WPS) void window_grad_kv_bf16(WindowGradArgs g
 }
 
 template <int D, int WPS>
-hipError_t run(const WindowGradArgs& g, hipStream_t st) {
+hipError_t run(const WindowGradArgs& args, hipStream_t st) {
+  WindowGradArgs g = args;
+  window_slots(&g.f, kBlock128);
   const unsigned q_grid = (unsigned)((g.f.w.Lq + kBlock128 - 1) / kBlock128 * g.f.w.B * g.f.w.Hq);
   if (q_grid) window_grad_q_bf16<D, WPS><<<q_grid, 256, 0, st>>>(g);
   if (g.blocks) window_grad_kv_bf16<D, WPS><<<window_pieces(g), 256, 0, st>>>(g);
