@@ -62,7 +62,8 @@ struct WindowGradArgs {
   const void* dout;
   void *dq, *dk, *dv;
   Strides3 sdo, sdq, sdk, sdv;
-  float* delta;  // a record per row [B, Hq, Lq]: fp32 the sum over the channels of dout * out; bf16 four floats (usv_window_grad.hip)
+  float* delta;  // a record per row [B, Hq, Lq]: fp32 the sum over the channels of dout * out; bf16 four planes (usv_window_grad.hip)
+  long long plane;
   // Key blocks are `block` keys.  Those below sink_blocks (every later row sees them) have sink_parts pieces, the others parts.
   int block, blocks, sink_blocks, sink_parts, parts;
   float* partial;  // dk, dv of the pieces: [slot][2][block][d]; a block in one piece has no slot

@@ -37,6 +37,9 @@ __device__ __forceinline__ void dma_scalar(unsigned lds, unsigned long long base
 __device__ __forceinline__ void dma_lane(unsigned lds, unsigned long long addr) {
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(addr) : "memory");
 }
+__device__ __forceinline__ void dma_dword(unsigned lds, unsigned long long addr) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" : : "s"(lds), "v"(addr) : "memory");
+}
 __device__ __forceinline__ unsigned long long uniform(unsigned long long x) {
   return ((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)x);
 }
@@ -54,17 +57,20 @@ __device__ __forceinline__ uint16_t* row_of(void* p, const Strides3& s, int b, i
 template <int D>
 struct Tile {
   static constexpr int LINES = D / 64, TENSOR = LINES * kLine, STAGE = 2 * TENSOR;
-  unsigned a_even, a_odd, b_even, b_odd;  // lane offsets in 8 rows
-  int wave, lane;
+  int wave;
   long long a_pitch, b_pitch;
-  __device__ __forceinline__ void init(int wave_, long long ap, long long bp) {
-    wave = wave_, lane = threadIdx.x & 63, a_pitch = ap, b_pitch = bp;
-    const unsigned chunk = ((lane & 7) ^ ((lane >> 4) << 1)) << 4;
-    a_even = (lane >> 3) * (unsigned)ap + chunk, a_odd = (lane >> 3) * (unsigned)ap + (chunk ^ 16);
-    b_even = (lane >> 3) * (unsigned)bp + chunk, b_odd = (lane >> 3) * (unsigned)bp + (chunk ^ 16);
+  __device__ __forceinline__ void init(int wave_, long long ap, long long bp) { wave = wave_, a_pitch = ap, b_pitch = bp; }
+  static __device__ __forceinline__ int lane_again() {  // (formed where it is used: once a tile, and registers are short)
+    int ln = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+    asm volatile("" : "+v"(ln));
+    return ln;
   }
   // rows row .. row + 63 of both
   __device__ __forceinline__ void load(unsigned lds, unsigned long long a, unsigned long long b, long long row) const {
+    const int lane = lane_again();
+    const unsigned chunk = ((lane & 7) ^ ((lane >> 4) << 1)) << 4;
+    const unsigned a_even = (lane >> 3) * (unsigned)a_pitch + chunk, a_odd = (lane >> 3) * (unsigned)a_pitch + (chunk ^ 16);
+    const unsigned b_even = (lane >> 3) * (unsigned)b_pitch + chunk, b_odd = (lane >> 3) * (unsigned)b_pitch + (chunk ^ 16);
     const unsigned long long a0 = a + (row + 16 * wave) * a_pitch, b0 = b + (row + 16 * wave) * b_pitch;
     const unsigned to = lds + 16 * wave * 128;
 #pragma unroll
@@ -82,6 +88,7 @@ struct Tile {
   template <typename F>
   __device__ __forceinline__ void load_rows(unsigned lds, unsigned long long a, unsigned long long b, F row_at) const {
     const unsigned to = lds + 16 * wave * 128;
+    const int lane = lane_again();
 #pragma unroll 1
     for (int r = 0; r < 2; ++r) {
       const long long row = row_at(16 * wave + 8 * r + (lane >> 3));
@@ -116,37 +123,44 @@ struct Lanes {
   }
 };
 
-// s (quarter 2 m + nt: rows 16 m + 4 G .. of the tile's 32, columns 16 nt + c) = rows of the tensor times the lane's columns
-template <int D>
-__device__ __forceinline__ f32x16 rows_times(const unsigned char* tensor, const Lanes& at, int sub, const bf16x8 (&f)[2][D / 32]) {
-  f32x16 s;
+// N fragments, each read kAhead places ahead of its products; the fences keep the order written here (left to itself the compiler reads a
+// fragment right in front of its products and waits for it).
+template <int N, int kAhead, typename Read, typename Use>
+__device__ __forceinline__ void pipeline(Read read, Use use) {
+  bf16x8 x[kAhead + 1];
 #pragma unroll
-  for (int t = 0; t < D / 32; ++t)
+  for (int f = 0; f < kAhead && f < N; ++f) x[f] = read(f);
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      const bf16x8 x = at.row_frag(tensor, sub, m, t);
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
-        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-        set_quarter(s, 2 * m + nt, __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, f[nt][t], t == 0 ? zero : quarter(s, 2 * m + nt), 0, 0, 0));
-      }
-    }
-  return s;
-}
-// o[nt][dt / 4] (quarter dt % 4: channels 16 dt + 4 G .., column 16 nt + c) += columns of the tensor times p
-template <int D>
-__device__ __forceinline__ void columns_times(const unsigned char* tensor, const Lanes& at, int sub, const bf16x8 (&p)[2], f32x16 (&o)[2][D / 64]) {
-#pragma unroll
-  for (int dt = 0; dt < D / 16; ++dt) {
-    const bf16x8 x = at.column_frag(tensor, sub, dt);
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
-      set_quarter(o[nt][dt >> 2], dt & 3, __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p[nt], quarter(o[nt][dt >> 2], dt & 3), 0, 0, 0));
+  for (int f = 0; f < N; ++f) {
+    if (f + kAhead < N) x[(f + kAhead) % (kAhead + 1)] = read(f + kAhead);
+    __builtin_amdgcn_sched_barrier(0);
+    use(f, x[f % (kAhead + 1)]);
+    __builtin_amdgcn_sched_barrier(0);
   }
+}
+// s (quarter 2 m + nt: rows 16 m + 4 G .. of the tile's 32, columns 16 nt + c) += a fragment of rows (m, t) times the lane's columns
+template <int KS>
+__device__ __forceinline__ void rows_times(f32x16& s, const bf16x8& x, int f, const bf16x8 (&col)[2][KS]) {
+  const int t = f >> 1, m = f & 1;
+#pragma unroll
+  for (int nt = 0; nt < 2; ++nt) {
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    set_quarter(s, 2 * m + nt, __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, col[nt][t], t == 0 ? zero : quarter(s, 2 * m + nt), 0, 0, 0));
+  }
+}
+// o[nt][dt / 4] (quarter dt % 4: channels 16 dt + 4 G .., column 16 nt + c) += a fragment of columns times p
+template <int OT>
+__device__ __forceinline__ void columns_times(f32x16 (&o)[2][OT], const bf16x8& x, int dt, const bf16x8 (&p)[2]) {
+#pragma unroll
+  for (int nt = 0; nt < 2; ++nt)
+    set_quarter(o[nt][dt >> 2], dt & 3, __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p[nt], quarter(o[nt][dt >> 2], dt & 3), 0, 0, 0));
+}
+template <int OT>
+__device__ __forceinline__ void pin(f32x16 (&o)[2][OT]) {  // in place (see quarter())
 #pragma unroll
   for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-    for (int x = 0; x < D / 64; ++x) asm volatile("" : "+v"(o[nt][x]));  // in place (see quarter())
+    for (int x = 0; x < OT; ++x) asm volatile("" : "+v"(o[nt][x]));
 }
 template <int D>
 __device__ __forceinline__ void clear(f32x16 (&o)[2][D / 64]) {
@@ -158,9 +172,12 @@ __device__ __forceinline__ void clear(f32x16 (&o)[2][D / 64]) {
       for (int r = 0; r < 16; ++r) o[nt][x][r] = 0.f;
 }
 
+__device__ __forceinline__ float at4(const float4& x, int r) { return r == 0 ? x.x : r == 1 ? x.y : r == 2 ? x.z : x.w; }
+
 template <int D, int WPS>
 __global__ __launch_bounds__(256, WPS) void window_grad_q_bf16(WindowGradArgs g) {
   using T = Tile<D>;
+  constexpr int NF = D / 16;  // row fragments of 32 rows
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * T::STAGE];
   const WindowArgs& a = g.f;
   const WindowSlot slot = window_slot(a, blockIdx.x, (a.w.Lq + kBlock128 - 1) / kBlock128);
@@ -208,7 +225,7 @@ __global__ __launch_bounds__(256, WPS) void window_grad_q_bf16(WindowGradArgs g)
       nlse[nt] = -a.lse[id] * kLog2e;
       range[nt] = window_range(a.w, seq.n, seq.first + some);
       if (G == 0 && row == some)
-        reinterpret_cast<float4*>(g.delta)[id] = make_float4(nlse[nt], delta[nt], __int_as_float(range[nt].lo), __int_as_float(range[nt].hi));
+        g.delta[id] = nlse[nt], g.delta[id + g.plane] = delta[nt], g.delta[id + 2 * g.plane] = __int_as_float(range[nt].lo), g.delta[id + 3 * g.plane] = __int_as_float(range[nt].hi);
     }
   }
   f32x16 dq[2][D / 64];
@@ -221,27 +238,39 @@ __global__ __launch_bounds__(256, WPS) void window_grad_q_bf16(WindowGradArgs g)
   for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) asm volatile("" : "+v"(qf[nt][t]), "+v"(dof[nt][t]));
-  for (int t = 0; t < tiles; ++t) {
+  // OPEN: every row of the block sees all keys of the tile
+  auto step = [&](auto open_c, int t) {
+    constexpr bool OPEN = decltype(open_c)::value;
     wait_vm<0>();
     __syncthreads();  // the tile is there; everybody is done with the other stage
     if (t + 1 < tiles) request(t + 1);
     const unsigned char* kt = smem + (t & 1) * T::STAGE;
     const unsigned char* vt = kt + T::TENSOR;
-    const bool open = window_tile_open(keys, t * kRows, kRows);
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub) {
-      f32x16 s = rows_times<D>(kt, at, sub, qf);
-      if (!open) {
+      f32x16 s, dp;
+      // S^T, then dP^T with the exponentials between its products
+      pipeline<2 * NF, 3>([&](int f) { return at.row_frag(f < NF ? kt : vt, sub, f & 1, f % NF >> 1); },
+                       [&](int f, const bf16x8& x) {
+                         if (f < NF) {
+                           rows_times(s, x, f, qf);
+                           return;
+                         }
+                         if (!OPEN && f == NF) {
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+                           for (int m = 0; m < 2; ++m)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int e = t * kRows + 32 * sub + 16 * m + 4 * G + r, key = window_key(keys, e);
+                             for (int r = 0; r < 4; ++r) {
+                               const int e = t * kRows + 32 * sub + 16 * m + 4 * G + r, key = window_key(keys, e);
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt) s[4 * (2 * m + nt) + r] = (e < keys.count) & window_sees(range[nt], a.w.sink, key) ? s[4 * (2 * m + nt) + r] : -INFINITY;
-          }
-      }
-      const f32x16 dp = rows_times<D>(vt, at, sub, dof);
+                               for (int nt = 0; nt < 2; ++nt)
+                                 s[4 * (2 * m + nt) + r] = (e < keys.count) & window_sees(range[nt], a.w.sink, key) ? s[4 * (2 * m + nt) + r] : -INFINITY;
+                             }
+                         }
+                         rows_times(dp, x, f - NF, dof);
+#pragma unroll
+                         for (int i = (f - NF) * 16 / NF; i < (f - NF + 1) * 16 / NF; ++i) s[i] = fast_exp2(fmaf(s[i], sl, nlse[i >> 2 & 1]));
+                       });
       bf16x8 ds[2];
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt)
@@ -250,10 +279,15 @@ __global__ __launch_bounds__(256, WPS) void window_grad_q_bf16(WindowGradArgs g)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int x = 4 * (2 * m + nt) + r;
-            ds[nt][4 * m + r] = (__bf16)(fast_exp2(fmaf(s[x], sl, nlse[nt])) * (dp[x] - delta[nt]));
+            ds[nt][4 * m + r] = (__bf16)(s[x] * (dp[x] - delta[nt]));
           }
-      columns_times<D>(kt, at, sub, ds, dq);
+      pipeline<D / 16, 3>([&](int f) { return at.column_frag(kt, sub, f); }, [&](int f, const bf16x8& x) { columns_times(dq, x, f, ds); });
+      pin(dq);
     }
+  };
+  for (int t = 0; t < tiles;) {
+    for (; t < tiles && window_tile_open(keys, t * kRows, kRows); ++t) step(std::true_type{}, t);
+    for (; t < tiles && !window_tile_open(keys, t * kRows, kRows); ++t) step(std::false_type{}, t);
   }
 #pragma unroll
   for (int nt = 0; nt < 2; ++nt) {
@@ -273,7 +307,8 @@ template <int D, int WPS>
 __global__ __launch_bounds__(256, WPS) void window_grad_kv_bf16(WindowGradArgs g) {
   using T = Tile<D>;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * T::STAGE];
-  __shared__ __attribute__((aligned(16))) float4 srow[2][kRows];  // -lse (log2 domain), D, lo, hi of a row
+  constexpr int KS = D / 32;
+  __shared__ __attribute__((aligned(16))) float srow[2][4][kRows];  // of every row -lse (log2 domain), D, lo, hi
   const WindowArgs& a = g.f;
   const WindowPiece pc = window_piece(g, blockIdx.x);
   const int k0 = pc.block * kBlock128;
@@ -309,10 +344,8 @@ __global__ __launch_bounds__(256, WPS) void window_grad_kv_bf16(WindowGradArgs g
       const unsigned to = lds + stage * T::STAGE;
       if (i + kRows <= i1) tile.load(to, qa, da, i);
       else tile.load_rows(to, qa, da, [&](int r) { return (long long)min(i + r, i1 - 1); });
-      if (wave == 0) {
-        const long long id = ((long long)pc.b * a.w.Hq + h) * a.w.Lq + min(i + lane, i1 - 1);
-        dma_lane(lds_row + stage * (kRows * 16), reinterpret_cast<unsigned long long>(reinterpret_cast<const float4*>(g.delta) + id));
-      }
+      const long long id = ((long long)pc.b * a.w.Hq + h) * a.w.Lq + min(i + lane, i1 - 1);
+      dma_dword(lds_row + (stage * 4 + wave) * (kRows * 4), reinterpret_cast<unsigned long long>(g.delta + wave * g.plane + id));
     };
     int h = pc.h * a.w.group, t = n0;
     if (n0 > 0) h += n0 / tiles, t = n0 % tiles;
@@ -344,7 +377,9 @@ __global__ __launch_bounds__(256, WPS) void window_grad_kv_bf16(WindowGradArgs g
     for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) asm volatile("" : "+v"(kf[nt][x]), "+v"(vf[nt][x]));
-    for (int n = n0; n < n1; ++n) {
+    // OPEN: every row of the tile sees every key of the block
+    auto step = [&](auto open_c, int n) {
+      constexpr bool OPEN = decltype(open_c)::value;
       wait_vm<0>();
       __syncthreads();
       const int i = i0 + t * kRows, stage = (n - n0) & 1;
@@ -352,50 +387,62 @@ __global__ __launch_bounds__(256, WPS) void window_grad_kv_bf16(WindowGradArgs g
       if (n + 1 < n1) request(h, t, stage ^ 1);
       const unsigned char* qt = smem + stage * T::STAGE;
       const unsigned char* dt = qt + T::TENSOR;
-      const bool open = i >= o0 && i + kRows <= o1;
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub) {
-        f32x16 s = rows_times<D>(qt, at, sub, kf);
-        if (!open) {
+        const float* rec = &srow[stage][0][32 * sub + 4 * G];
+        f32x4 s[2][2], dp[2][2];  // [m][nt]
+        bf16x8 p[2], ds[2];
+        float4 nlse;
+        auto weigh = [&](int m) {  // P and dS of 16 rows, in bf16
+          const float4 del = *reinterpret_cast<const float4*>(rec + kRows + 16 * m);
 #pragma unroll
-          for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int x = 32 * sub + 16 * m + 4 * G + r;
-              const float4 rec = srow[stage][x];
-              const WindowRange range = {__float_as_int(rec.z), i + x < i1 ? __float_as_int(rec.w) : 0};
-#pragma unroll
-              for (int nt = 0; nt < 2; ++nt) s[4 * (2 * m + nt) + r] = window_sees(range, a.w.sink, key0 + 16 * nt) ? s[4 * (2 * m + nt) + r] : -INFINITY;
-            }
-        }
-        float del[2][4];
-        bf16x8 p[2];
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float2 rec = *reinterpret_cast<const float2*>(&srow[stage][32 * sub + 16 * m + 4 * G + r]);
-            del[m][r] = rec.y;
-#pragma unroll
-            for (int nt = 0; nt < 2; ++nt) {
-              const int x = 4 * (2 * m + nt) + r;
-              s[x] = fast_exp2(fmaf(s[x], sl, rec.x));
-              p[nt][4 * m + r] = (__bf16)s[x];
-            }
-          }
-        columns_times<D>(dt, at, sub, p, dv);
-        const f32x16 dp = rows_times<D>(dt, at, sub, vf);
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-          for (int m = 0; m < 2; ++m)
+          for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              const int x = 4 * (2 * m + nt) + r;
-              p[nt][4 * m + r] = (__bf16)(s[x] * (dp[x] - del[m][r]));
+              p[nt][4 * m + r] = (__bf16)s[m][nt][r];
+              ds[nt][4 * m + r] = (__bf16)(s[m][nt][r] * (dp[m][nt][r] - at4(del, r)));
             }
-        columns_times<D>(qt, at, sub, p, dk);
+        };
+        // 16 rows at a time: S, then dP with the exponentials between its products
+        pipeline<4 * KS, 1>([&](int f) { return at.row_frag(f % (2 * KS) < KS ? qt : dt, sub, f / (2 * KS), f % KS); },
+                            [&](int f, const bf16x8& x) {
+                              const int m = f / (2 * KS), g = f % (2 * KS), t = f % KS;
+                              if (!OPEN && g == KS) {
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) {
+                                  const int row = i + 32 * sub + 16 * m + 4 * G + r;
+                                  const WindowRange range = {__float_as_int(rec[2 * kRows + 16 * m + r]), __float_as_int(rec[3 * kRows + 16 * m + r])};
+#pragma unroll
+                                  for (int nt = 0; nt < 2; ++nt) s[m][nt][r] = (row < i1) & window_sees(range, a.w.sink, key0 + 16 * nt) ? s[m][nt][r] : -INFINITY;
+                                }
+                              }
+                              if (g == KS - 1) nlse = *reinterpret_cast<const float4*>(rec + 16 * m);
+#pragma unroll
+                              for (int nt = 0; nt < 2; ++nt) {
+                                const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+                                if (g < KS) s[m][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, kf[nt][t], t == 0 ? zero : s[m][nt], 0, 0, 0);
+                                else dp[m][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, vf[nt][t], t == 0 ? zero : dp[m][nt], 0, 0, 0);
+                              }
+                              if (g >= KS) {
+#pragma unroll
+                                for (int e = (g - KS) * 8 / KS; e < (g - KS + 1) * 8 / KS; ++e) s[m][e >> 2][e & 3] = fast_exp2(fmaf(s[m][e >> 2][e & 3], sl, at4(nlse, e & 3)));
+                              }
+                              if (m == 0 && g == 2 * KS - 1) weigh(0);
+                            });
+        weigh(1);
+        pipeline<2 * (D / 16), 2>([&](int f) { return at.column_frag(f < D / 16 ? dt : qt, sub, f % (D / 16)); },
+                                  [&](int f, const bf16x8& x) {
+                                    if (f < D / 16) columns_times(dv, x, f, p);
+                                    else columns_times(dk, x, f - D / 16, ds);
+                                  });
+        pin(dv);
+        pin(dk);
       }
+    };
+    auto open = [&]() { return i0 + t * kRows >= o0 && i0 + t * kRows + kRows <= o1; };
+    for (int n = n0; n < n1;) {
+      for (; n < n1 && open(); ++n) step(std::true_type{}, n);
+      for (; n < n1 && !open(); ++n) step(std::false_type{}, n);
     }
   }
   const int key0 = k0 + 32 * wave + c;
@@ -427,6 +474,7 @@ template <int D, int WPS>
 hipError_t run(const WindowGradArgs& args, hipStream_t st) {
   WindowGradArgs g = args;
   window_slots(&g.f, kBlock128);
+  g.plane = (long long)g.f.w.B * g.f.w.Hq * g.f.w.Lq;
   const unsigned q_grid = (unsigned)((g.f.w.Lq + kBlock128 - 1) / kBlock128 * g.f.w.B * g.f.w.Hq);
   if (q_grid) window_grad_q_bf16<D, WPS><<<q_grid, 256, 0, st>>>(g);
   if (g.blocks) window_grad_kv_bf16<D, WPS><<<window_pieces(g), 256, 0, st>>>(g);
