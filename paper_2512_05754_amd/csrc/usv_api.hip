@@ -289,6 +289,18 @@ int cache_attn_splits(const usv::WindowShape& s) {
   return n < 2 ? 1 : n > 256 ? 256 : (int)n;
 }
 
+// cache_attn of many rows takes the keys that they see out of the cache, in bf16, and runs window_attn's kernel on them: the codes are
+// converted once and not once per 64 rows.  Rows of that copy; 0: the kernel that reads codes.
+long long cache_attn_copy(const usv::CacheShape& c, const usv::WindowShape& s) {
+  const long long rows = window_most_keys(s, s.Lq), bytes = 4 * rows * s.B * s.Hkv * c.d;
+  return (long long)s.Lq * s.group >= 1024 && bytes <= (1LL << 30) ? rows : 0;
+}
+size_t cache_attn_copy_bytes(const usv::CacheShape& c, long long rows) { return (size_t)4 * rows * c.B * c.H * c.d; }
+size_t cache_attn_bytes(const usv::CacheShape& c, const usv::WindowShape& s) {
+  const long long rows = cache_attn_copy(c, s);
+  return rows ? cache_attn_copy_bytes(c, rows) + window_part_bytes(s, c.d, window_splits(s, c.d)) : window_part_bytes(s, c.d, cache_attn_splits(s));
+}
+
 #define USV_TRY(expr)                    \
   do {                                   \
     const usv_status st__ = (expr);      \
@@ -927,7 +939,7 @@ size_t usv_cache_attn_workspace_bytes(const usv_cache* c, const usv_window* w) {
   usv::CacheShape s;
   usv::WindowShape ws;
   if (check_cache_attn(c, w, &s, &ws) != USV_OK) return 0;
-  return window_part_bytes(ws, s.d, cache_attn_splits(ws));
+  return cache_attn_bytes(s, ws);
 }
 
 usv_status usv_cache_attn(const void* q, const void* cache, const usv_cache* c, const usv_window* w, float scale, void* out,
@@ -946,21 +958,32 @@ usv_status usv_cache_attn(const void* q, const void* cache, const usv_cache* c, 
     if (lse) USV_TRY(check_ptr(lse, "lse"));
   }
   if (!(scale <= 0.f) && !std::isfinite(scale)) return fail(USV_ERR_INVALID_ARG, "scale must be finite");
-  int splits = cache_attn_splits(a.f.w);
-  if (!ws) splits = 1;
-  else {
+  const size_t need = cache_attn_bytes(a.c, a.f.w);
+  if (ws) {
     USV_TRY(check_ptr(ws, "ws"));
-    if (ws_bytes < window_part_bytes(a.f.w, d, splits))
-      return fail(USV_ERR_WORKSPACE, "ws holds %zu bytes, %zu are needed", ws_bytes, window_part_bytes(a.f.w, d, splits));
+    if (ws_bytes < need) return fail(USV_ERR_WORKSPACE, "ws holds %zu bytes, %zu are needed", ws_bytes, need);
   }
   a.cache = static_cast<const unsigned char*>(cache);
   a.f.q = q, a.f.out = out, a.f.lse = lse;
   a.f.scale = scale > 0.f ? scale : 1.f / std::sqrt((float)d);
-  window_set_parts(&a.f, d, splits, ws);
   if (w->q_len == 0) return hip_result(hipSuccess, "");
   hipStream_t st = static_cast<hipStream_t>(stream);
-  hipError_t e = usv::launch_cache_attn(a, st);
-  if (e == hipSuccess && splits > 1) e = usv::launch_window_join(a.f, true, d, st);
+  const long long copy = ws ? cache_attn_copy(a.c, a.f.w) : 0;
+  hipError_t e;
+  if (copy) {
+    usv::CacheRowsArgs r = {};
+    r.c = a.c, r.cache = const_cast<unsigned char*>(a.cache), r.rows = (int)copy;
+    r.sk = r.sv = {2LL * copy * d * a.c.H, 2LL * copy * d, 2LL * d};
+    r.k = ws, r.v = static_cast<unsigned char*>(ws) + cache_attn_copy_bytes(a.c, copy) / 2;
+    a.f.k = r.k, a.f.v = r.v, a.f.sk = r.sk, a.f.sv = r.sv, a.f.compact = 1;
+    window_set_parts(&a.f, d, window_splits(a.f.w, d), static_cast<unsigned char*>(ws) + cache_attn_copy_bytes(a.c, copy));
+    e = usv::launch_cache_expand(r, a.f.w, st);
+    if (e == hipSuccess) e = usv::launch_window_bf16(a.f, d, st);
+  } else {
+    window_set_parts(&a.f, d, ws ? cache_attn_splits(a.f.w) : 1, ws);
+    e = usv::launch_cache_attn(a, st);
+  }
+  if (e == hipSuccess && a.f.splits > 1) e = usv::launch_window_join(a.f, true, d, st);
   return hip_result(e, "usv_cache_attn");
 }
 

@@ -39,6 +39,8 @@ hipError_t launch_cache_write(const CacheRowsArgs& a, bool bf16, hipStream_t st)
 hipError_t launch_cache_read(const CacheRowsArgs& a, bool bf16, hipStream_t st);
 // query rows (tokens x the heads that share a key head) of a workgroup: 16, or 64 where that many are at hand
 inline int cache_attn_rows(const WindowShape& w) { return (long long)w.Lq * w.group > 32 ? 64 : 16; }
+// the keys that some query row sees (window_all_keys), in bf16, to k, v [B, heads, rows, d] of a
+hipError_t launch_cache_expand(const CacheRowsArgs& a, const WindowShape& w, hipStream_t st);
 hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t st);
 
 }  // namespace usv

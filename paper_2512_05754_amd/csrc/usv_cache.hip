@@ -44,14 +44,7 @@ struct Place {
   long long page;  // < 0: no such page
   int row;
 };
-template <int D>
-__device__ __forceinline__ bool place_of(const CacheRowsArgs& a, Place* p) {
-  constexpr int PER = D / 8;
-  const long long i = (long long)blockIdx.x * (256 / PER) + threadIdx.x / PER;
-  if (i >= a.rows) return false;
-  p->i = (int)i, p->h = blockIdx.y, p->b = blockIdx.z;
-  if (a.counts && p->i >= a.counts[p->b]) return false;
-  const long long pos = (long long)a.starts[p->b] + p->i;
+__device__ __forceinline__ void place_at(const CacheRowsArgs& a, long long pos, Place* p) {
   p->page = -1, p->row = 0;
   if (pos >= 0 && pos < (long long)a.c.table_pages * a.c.page_size) {
     const int slot = (int)pos / a.c.by_page;
@@ -59,6 +52,16 @@ __device__ __forceinline__ bool place_of(const CacheRowsArgs& a, Place* p) {
     const int page = a.c.table[(long long)p->b * a.c.table_pages + slot];
     if (page >= 0 && page < a.c.pages) p->page = page;
   }
+}
+
+template <int D>
+__device__ __forceinline__ bool place_of(const CacheRowsArgs& a, Place* p) {
+  constexpr int PER = D / 8;
+  const long long i = (long long)blockIdx.x * (256 / PER) + threadIdx.x / PER;
+  if (i >= a.rows) return false;
+  p->i = (int)i, p->h = blockIdx.y, p->b = blockIdx.z;
+  if (a.counts && p->i >= a.counts[p->b]) return false;
+  place_at(a, (long long)a.starts[p->b] + p->i, p);
   return true;
 }
 
@@ -107,10 +110,8 @@ __global__ __launch_bounds__(256) void cache_write(CacheRowsArgs a) {
 }
 
 template <typename T, int D, int BITS>
-__global__ __launch_bounds__(256) void cache_read(CacheRowsArgs a) {
+__device__ __forceinline__ void read_row(const CacheRowsArgs& a, const Place& p) {
   constexpr int PER = D / 8, CB = D * BITS / 8, SB = D / 32;
-  Place p;
-  if (!place_of<D>(a, &p)) return;
   const int t = threadIdx.x % PER;
   const unsigned char* base = a.cache + (max(p.page, 0LL) * a.c.H + p.h) * a.c.head_bytes();
   uint2 raw[2] = {};
@@ -151,6 +152,21 @@ __global__ __launch_bounds__(256) void cache_read(CacheRowsArgs a) {
     }
   }
 }
+template <typename T, int D, int BITS>
+__global__ __launch_bounds__(256) void cache_read(CacheRowsArgs a) {
+  Place p;
+  if (place_of<D>(a, &p)) read_row<T, D, BITS>(a, p);
+}
+template <int D, int BITS>
+__global__ __launch_bounds__(256) void cache_expand(CacheRowsArgs a, WindowShape w) {
+  constexpr int PER = D / 8;
+  Place p;
+  p.i = blockIdx.x * (256 / PER) + threadIdx.x / PER, p.h = blockIdx.y, p.b = blockIdx.z;
+  const WindowKeys keys = window_all_keys(w, window_seq_of(w, p.b));
+  if (p.i >= min(keys.count, a.rows)) return;
+  place_at(a, window_key(keys, p.i), &p);
+  read_row<uint16_t, D, BITS>(a, p);
+}
 
 template <typename F>
 hipError_t by_kind(const CacheRowsArgs& a, bool bf16, F f) {
@@ -179,6 +195,12 @@ hipError_t launch_cache_write(const CacheRowsArgs& a, bool bf16, hipStream_t st)
 hipError_t launch_cache_read(const CacheRowsArgs& a, bool bf16, hipStream_t st) {
   return by_kind(a, bf16, [&](auto t, auto d, auto bits, const dim3& grid) {
     cache_read<decltype(t), decltype(d)::value, decltype(bits)::value><<<grid, 256, 0, st>>>(a);
+  });
+}
+
+hipError_t launch_cache_expand(const CacheRowsArgs& a, const WindowShape& w, hipStream_t st) {
+  return by_kind(a, true, [&](auto t, auto d, auto bits, const dim3& grid) {
+    if constexpr (std::is_same<decltype(t), uint16_t>::value) cache_expand<decltype(d)::value, decltype(bits)::value><<<grid, 256, 0, st>>>(a, w);
   });
 }
 

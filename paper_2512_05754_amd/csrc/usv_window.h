@@ -49,7 +49,8 @@ struct WindowArgs {
   float scale;
   int splits;  // > 1: the key list is shared out, results go to part_o [splits][rows][d] (normalised, fp32) and part_lse [splits][rows]
   float *part_o, *part_lse;
-  int period;  // bf16 kernel: see there
+  int period;   // bf16 kernel: see there
+  int compact;  // bf16 kernel: k and v hold the keys of window_keys for all query rows, one behind the other, instead of all positions
   Div by_items, by_rest, by_period;  // window_slot; period
 };
 // What window_slot needs for blocks of `rows` query rows.
@@ -208,6 +209,9 @@ __device__ __forceinline__ WindowPiece window_piece(const WindowGradArgs& g, int
 constexpr int kWindowRows = 64;  // query rows of a workgroup
 
 hipError_t launch_window_f32(const WindowArgs& a, int d, hipStream_t st);
+// The keys that some query row sees, as a list (compact).
+__host__ __device__ inline WindowKeys window_all_keys(const WindowShape& w, const WindowSeq& s) { return window_keys(w, s, 0, w.Lq); }
+
 hipError_t launch_window_bf16(const WindowArgs& a, int d, hipStream_t st);
 hipError_t launch_window_join(const WindowArgs& a, bool bf16, int d, hipStream_t st);
 hipError_t launch_window_grad_f32(const WindowGradArgs& a, int d, hipStream_t st);

@@ -141,6 +141,9 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   }
 
   const int hk = __builtin_amdgcn_readfirstlane(slot.h / w.by_group);
+  // rows of k and v that lie ahead of a key of the window (one of the sinks: key) but are not there
+  const int gone = a.compact ? __builtin_amdgcn_readfirstlane(window_all_keys(w, seq).skip) : 0;
+  auto row_at = [&](int entry) { return (long long)(entry < keys.head ? entry : entry + keys.skip - gone); };
   const unsigned wave_lds = lds_address(smem) + wave * kWaveBytes;
   // DMA lane -> row lane / 8 of an instruction's 8 rows, 16-byte chunk lane % 8 of the line; K chunks are stored at chunk ^ (row / 2 % 8), V
   // chunks at chunk ^ 2 (row / 2 % 4)
@@ -150,7 +153,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   // rows 8 r of the step to be requested next, short of what the instruction's offset field adds
   unsigned long long kb[4], vb[4];
   auto point_at = [&](int entry) {
-    const long long key = window_key(keys, entry);
+    const long long key = row_at(entry);
     const ArgsAgain b = again();
     const unsigned long long kb0 = reinterpret_cast<unsigned long long>(b->k) + slot.b * b->sk.batch + hk * b->sk.head;
     const unsigned long long vb0 = reinterpret_cast<unsigned long long>(b->v) + slot.b * b->sv.batch + hk * b->sv.head;
@@ -181,7 +184,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
     for (int x = 0; x < IPS; ++x)
 #pragma unroll 1
       for (int r = 0; r < 4; ++r) {
-        const long long key = window_key(keys, max(e + 8 * r + (ln >> 3), 0));
+        const long long key = row_at(max(e + 8 * r + (ln >> 3), 0));
         const unsigned kc = ((ln & 7) ^ (((4 * r) & 7) ^ (ln >> 4))) << 4, vc = ((ln & 7) ^ (((ln >> 4) & 3) << 1)) << 4;
         dma_lane(wave_lds + x * kItem + 1024 * r, (x < LINES ? kb0 + key * b->sk.token + kc : vb0 + key * b->sv.token + vc) + x % LINES * 128);
       }

@@ -188,6 +188,11 @@ DECODES = [
     Decode(1, 3, 1, 50, 224, 64, 4, 32, [200], -1, -1),                   # both ways, 150 rows
     Decode(2, 2, 1, 70, 256, 128, 8, 64, [256, 71], 0, 1, 0, 16),
     Decode(1, 1, 1, 1, 640, 64, 4, 64, [600], 0, 0, 0),                   # sees itself only
+    # 1024 rows a key head and more: the keys that they see are taken out first
+    Decode(2, 4, 1, 300, 960, 128, 4, 64, [960, 310], 1, 0, 1, 150),
+    Decode(1, 1, 1, 1100, 2560, 64, 8, 16, [2500], 100, 0, 3),
+    Decode(1, 2, 1, 520, 640, 128, 8, 64, [600]),
+    Decode(2, 8, 2, 256, 2048, 64, 4, 256, [2000, 0], 1, 0, 2, 128),
 ]
 
 
@@ -212,6 +217,10 @@ def test_attention_over_the_cache(usv, c):
     out, lse = usv.cache_attn(q.to(DEV), cache, t.to(DEV), ints(c.lens), **c.args, bits=c.bits, return_lse=True)
     close(out, ref, mag, "bf16", "out")
     close_lse(lse, lse_ref)
+    if c.Lq * (c.Hq // c.Hkv) >= 1024:  # without scratch the codes are read where they lie
+        out2, lse2 = usv.cache_attn(q.to(DEV), cache, t.to(DEV), ints(c.lens), **c.args, bits=c.bits, return_lse=True, workspace=torch.empty(0, dtype=torch.uint8, device=DEV))
+        close(out2, ref, mag, "bf16", "out")
+        close_lse(lse2, lse_ref)
     # queries as a projection lays them out, the output into such a view: the same bits
     buf = torch.full((c.B, c.Lq, c.Hq, c.d + 8), 7.0, dtype=q.dtype, device=DEV)
     qs = q.transpose(1, 2).contiguous().transpose(1, 2).to(DEV)
