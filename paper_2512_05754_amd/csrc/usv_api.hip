@@ -179,15 +179,20 @@ long long window_most_keys(const usv::WindowShape& s, int rows) {
   return n < s.Lk ? n : s.Lk;
 }
 
-// Pieces that the key list of a block of rows is shared out in: enough to fill the chip, eight tiles of 64 keys each at least
-// (a piece is a workgroup of its own and 64 fp32 rows through memory).
-int window_splits(const usv::WindowShape& s, int d) {
-  const long long wgs = (long long)((s.Lq + usv::kWindowRows - 1) / usv::kWindowRows) * s.B * s.Hq;
-  const long long slots = d == 128 ? 1024 : 1536, tiles = (window_most_keys(s, usv::kWindowRows) + 63) / 64;
+// Pieces that the key lists of blocks of `rows` query rows are shared out in: enough to fill the chip, which runs `slots` workgroups
+// together, `least` keys each at least (a piece is a workgroup of its own, and its rows go through memory in fp32).
+int window_pieces_of(const usv::WindowShape& s, int rows, long long slots, int least) {
+  const long long wgs = (long long)((s.Lq + rows - 1) / rows) * s.B * s.Hq;
   if (wgs == 0 || 2 * wgs > slots) return 1;
-  const long long by_slots = slots / wgs, by_tiles = tiles / 8;
-  const long long n = by_slots < by_tiles ? by_slots : by_tiles;
+  const long long by_slots = slots / wgs, by_keys = window_most_keys(s, rows) / least;
+  const long long n = by_slots < by_keys ? by_slots : by_keys;
   return n < 2 ? 1 : n > 256 ? 256 : (int)n;
+}
+int window_splits(const usv::WindowShape& s, int d, bool bf16) {
+  return bf16 ? window_pieces_of(s, usv::kWindowRows, d == 128 ? 1024 : 1536, 512) : window_pieces_of(s, usv::kWindowRows, 768, 256);
+}
+int window_grad_splits(const usv::WindowShape& s, int d, bool bf16) {
+  return bf16 ? window_pieces_of(s, 128, d == 128 ? 512 : 768, 512) : window_pieces_of(s, usv::kWindowRows, 512, 256);
 }
 size_t window_part_bytes(const usv::WindowShape& s, int d, int splits) {
   return splits > 1 ? (size_t)splits * s.B * s.Hq * s.Lq * (d + 4) * sizeof(float) : 0;  // (d + 1, kept aligned)
@@ -227,6 +232,7 @@ size_t window_partial_bytes(const usv::WindowGradArgs& g, int d) {
   const size_t slots = heads * ((g.sink_parts > 1 ? (size_t)g.sink_blocks * g.sink_parts : 0) + (g.parts > 1 ? (size_t)(g.blocks - g.sink_blocks) * g.parts : 0));
   return slots * 2 * g.block * d * sizeof(float);
 }
+size_t window_dq_bytes(const usv::WindowShape& s, int d, int splits) { return splits > 1 ? (size_t)splits * s.B * s.Hq * s.Lq * d * sizeof(float) : 0; }
 void window_grad_plan_for(usv::WindowGradArgs* g, const usv_window* w) {  // (workgroups: what the chip runs together)
   if (w->dtype == USV_BF16) window_grad_plan(g, 128, 64, w->head_dim == 128 ? 512 : 768);
   else window_grad_plan(g, 64, 32, w->head_dim == 128 ? 512 : 768);
@@ -290,7 +296,9 @@ int cache_attn_splits(const usv::WindowShape& s) {
 }
 
 // cache_attn of many rows takes the keys that they see out of the cache, in bf16, and runs window_attn's kernel on them: the codes are
-// converted once and not once per 64 rows.  Rows of that copy; 0: the kernel that reads codes.
+// converted once and not once per 64 rows.  Rows of that copy; 0: the kernel that reads codes.  With codes / with the copy, d = 128: 12 key heads of
+// 15600 keys in 8 bits, 256 rows 54 / 72 us, 512 84 / 91, 1024 174 / 130, 4680 657 / 500; in 4 bits, 512 74 / 87, 1024 151 / 125; 4 x 8 key heads of 8192
+// keys, 512 rows 92 / 108, 1024 152 / 164; d = 64: 2 x 16 key heads, 512 rows 73 / 72.  Copies beyond 1 GiB are not made.
 long long cache_attn_copy(const usv::CacheShape& c, const usv::WindowShape& s) {
   const long long rows = window_most_keys(s, s.Lq), bytes = 4 * rows * s.B * s.Hkv * c.d;
   return (long long)s.Lq * s.group >= 1024 && bytes <= (1LL << 30) ? rows : 0;
@@ -298,7 +306,7 @@ long long cache_attn_copy(const usv::CacheShape& c, const usv::WindowShape& s) {
 size_t cache_attn_copy_bytes(const usv::CacheShape& c, long long rows) { return (size_t)4 * rows * c.B * c.H * c.d; }
 size_t cache_attn_bytes(const usv::CacheShape& c, const usv::WindowShape& s) {
   const long long rows = cache_attn_copy(c, s);
-  return rows ? cache_attn_copy_bytes(c, rows) + window_part_bytes(s, c.d, window_splits(s, c.d)) : window_part_bytes(s, c.d, cache_attn_splits(s));
+  return rows ? cache_attn_copy_bytes(c, rows) + window_part_bytes(s, c.d, window_splits(s, c.d, true)) : window_part_bytes(s, c.d, cache_attn_splits(s));
 }
 
 #define USV_TRY(expr)                    \
@@ -806,7 +814,7 @@ usv_status usv_cube_scatter(const void* cube, const usv_shape* shape, const usv_
 size_t usv_window_workspace_bytes(const usv_window* w) {
   usv::WindowShape s;
   if (check_window(w, &s) != USV_OK) return 0;
-  return window_part_bytes(s, w->head_dim, window_splits(s, w->head_dim));
+  return window_part_bytes(s, w->head_dim, window_splits(s, w->head_dim, w->dtype == USV_BF16));
 }
 
 usv_status usv_window_attn(const void* q, const void* k, const void* v, const usv_window* w, float scale, void* out,
@@ -830,7 +838,7 @@ usv_status usv_window_attn(const void* q, const void* k, const void* v, const us
     if (lse) USV_TRY(check_ptr(lse, "lse"));
   }
   if (!(scale <= 0.f) && !std::isfinite(scale)) return fail(USV_ERR_INVALID_ARG, "scale must be finite");
-  int splits = window_splits(a.w, d);
+  int splits = window_splits(a.w, d, bf16);
   if (!ws) splits = 1;
   else {
     USV_TRY(check_ptr(ws, "ws"));
@@ -851,7 +859,9 @@ size_t usv_window_backward_workspace_bytes(const usv_window* w) {
   usv::WindowGradArgs g = {};
   if (check_window(w, &g.f.w) != USV_OK) return 0;
   window_grad_plan_for(&g, w);
-  const size_t n = window_delta_bytes(g.f.w, w->dtype == USV_BF16) + window_partial_bytes(g, w->head_dim);
+  const bool bf16 = w->dtype == USV_BF16;
+  const size_t n = window_delta_bytes(g.f.w, bf16) + window_partial_bytes(g, w->head_dim) +
+                   window_dq_bytes(g.f.w, w->head_dim, window_grad_splits(g.f.w, w->head_dim, bf16));
   return n ? n : 16;
 }
 
@@ -889,7 +899,8 @@ usv_status usv_window_attn_backward(const void* q, const void* k, const void* v,
   if (!(scale <= 0.f) && !std::isfinite(scale)) return fail(USV_ERR_INVALID_ARG, "scale must be finite");
   window_grad_plan_for(&g, w);
   USV_TRY(check_ptr(ws, "ws"));
-  const size_t need = window_delta_bytes(a.w, bf16) + window_partial_bytes(g, d);
+  g.q_splits = window_grad_splits(a.w, d, bf16);
+  const size_t need = window_delta_bytes(a.w, bf16) + window_partial_bytes(g, d) + window_dq_bytes(a.w, d, g.q_splits);
   if (ws_bytes < need) return fail(USV_ERR_WORKSPACE, "ws holds %zu bytes, %zu are needed", ws_bytes, need);
   a.q = q, a.k = k, a.v = v, a.out = const_cast<void*>(out), a.lse = const_cast<float*>(lse);
   a.scale = scale > 0.f ? scale : 1.f / std::sqrt((float)d);
@@ -897,8 +908,10 @@ usv_status usv_window_attn_backward(const void* q, const void* k, const void* v,
   g.dout = dout, g.dq = dq, g.dk = dk, g.dv = dv;
   g.delta = static_cast<float*>(ws);
   g.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + window_delta_bytes(a.w, bf16));
+  g.dq_part = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(g.partial) + window_partial_bytes(g, d));
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e = bf16 ? usv::launch_window_grad_bf16(g, d, st) : usv::launch_window_grad_f32(g, d, st);
+  if (e == hipSuccess && g.q_splits > 1) e = usv::launch_window_grad_q_join(g, bf16, d, st);
   if (e == hipSuccess && window_partial_bytes(g, d)) e = usv::launch_window_grad_join(g, bf16, d, st);
   return hip_result(e, "usv_window_attn_backward");
 }
@@ -976,7 +989,7 @@ usv_status usv_cache_attn(const void* q, const void* cache, const usv_cache* c, 
     r.sk = r.sv = {2LL * copy * d * a.c.H, 2LL * copy * d, 2LL * d};
     r.k = ws, r.v = static_cast<unsigned char*>(ws) + cache_attn_copy_bytes(a.c, copy) / 2;
     a.f.k = r.k, a.f.v = r.v, a.f.sk = r.sk, a.f.sv = r.sv, a.f.compact = 1;
-    window_set_parts(&a.f, d, window_splits(a.f.w, d), static_cast<unsigned char*>(ws) + cache_attn_copy_bytes(a.c, copy));
+    window_set_parts(&a.f, d, window_splits(a.f.w, d, true), static_cast<unsigned char*>(ws) + cache_attn_copy_bytes(a.c, copy));
     e = usv::launch_cache_expand(r, a.f.w, st);
     if (e == hipSuccess) e = usv::launch_window_bf16(a.f, d, st);
   } else {

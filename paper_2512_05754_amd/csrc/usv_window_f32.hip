@@ -245,7 +245,9 @@ __global__ __launch_bounds__(256) void window_grad_q(WindowGradArgs g) {
   f32x4 dq[D / 16];
 #pragma unroll
   for (int dt = 0; dt < D / 16; ++dt) dq[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (tiles > 0) {
+  int t0 = 0, t1 = tiles;
+  if (g.q_splits > 1) t0 = (int)((long long)tiles * blockIdx.y / g.q_splits), t1 = (int)((long long)tiles * (blockIdx.y + 1) / g.q_splits);
+  if (tiles > 0) {  // (also of a piece without tiles: the first one leaves D)
     const int qrow = min(max(row, keys.i0), keys.i1 - 1);
     const WindowRange range = window_range(a.w, seq.n, seq.first + qrow);
     float4 qf[D / 16], dof[D / 16];
@@ -261,19 +263,19 @@ __global__ __launch_bounds__(256) void window_grad_q(WindowGradArgs g) {
       delta += dof[u].x * of.x + dof[u].y * of.y + dof[u].z * of.z + dof[u].w * of.w;
     }
     delta = sum_over_groups(delta);
-    if (G == 0 && live) g.delta[id] = delta;
+    if (G == 0 && live && blockIdx.y == 0) g.delta[id] = delta;
     const float sl = a.scale * kLog2e, ref = a.lse[((long long)at_.b * a.w.Hq + at_.h) * a.w.Lq + qrow] * kLog2e;
     Pair<T, D> next;
     auto fetch = [&](int t) {
       const long long key = window_key(keys, min(t * kTile + (int)(threadIdx.x >> 3), keys.count - 1));
       next.load(row_of<T>(a.k, a.sk, at_.b, hk, key), row_of<T>(a.v, a.sv, at_.b, hk, key));
     };
-    fetch(0);
-    for (int t = 0; t < tiles; ++t) {
+    if (t0 < t1) fetch(t0);
+    for (int t = t0; t < t1; ++t) {
       __syncthreads();
       next.store(sk, sv);
       __syncthreads();
-      if (t + 1 < tiles) fetch(t + 1);
+      if (t + 1 < t1) fetch(t + 1);
       f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, dp[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
       rows_times<D>(sk, qf, s);
       rows_times<D>(sv, dof, dp);
@@ -290,6 +292,12 @@ __global__ __launch_bounds__(256) void window_grad_q(WindowGradArgs g) {
     }
   }
   if (row >= a.w.Lq) return;
+  if (g.q_splits > 1) {
+    float* part = g.dq_part + (blockIdx.y * ((long long)a.w.B * a.w.Hq * a.w.Lq) + id) * D + 4 * G;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) put4<float>(part + 16 * dt, live ? make_float4(dq[dt][0], dq[dt][1], dq[dt][2], dq[dt][3]) : make_float4(0.f, 0.f, 0.f, 0.f));
+    return;
+  }
   T* dst = row_of<T>(g.dq, g.sdq, at_.b, at_.h, row);
 #pragma unroll
   for (int dt = 0; dt < D / 16; ++dt) {
@@ -406,6 +414,24 @@ __global__ __launch_bounds__(256) void window_grad_join(WindowGradArgs g) {
   put4<T>(row_of<T>(g.dv, g.sdv, b, h, key) + ch, dv);
 }
 
+// dq of a row = sum of its pieces, in their order.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void window_grad_q_join(WindowGradArgs g) {
+  const WindowArgs& a = g.f;
+  const long long rows = (long long)a.w.B * a.w.Hq * a.w.Lq;
+  const long long id = (long long)blockIdx.x * (1024 / D) + threadIdx.x / (D / 4);
+  if (id >= rows) return;
+  const int ch = 4 * (threadIdx.x % (D / 4));
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int s = 0; s < g.q_splits; ++s) {
+    const float4 x = load4(g.dq_part + (s * rows + id) * D + ch);
+    sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
+  }
+  const int row = (int)(id % a.w.Lq), bh = (int)(id / a.w.Lq);
+  put4<T>(row_of<T>(g.dq, g.sdq, bh / a.w.Hq, bh % a.w.Hq, row) + ch, make_float4(sum.x * a.scale, sum.y * a.scale, sum.z * a.scale, sum.w * a.scale));
+}
+
 template <typename F>
 hipError_t by_type(bool bf16, int d, F f) {
   if (bf16) d == 128 ? f(uint16_t{}, std::integral_constant<int, 128>{}) : f(uint16_t{}, std::integral_constant<int, 64>{});
@@ -438,7 +464,7 @@ hipError_t launch_window_grad_f32(const WindowGradArgs& args, int d, hipStream_t
   const unsigned q_grid = (unsigned)((g.f.w.Lq + kWindowRows - 1) / kWindowRows * g.f.w.B * g.f.w.Hq);
   auto go = [&](auto dc) {
     constexpr int D = decltype(dc)::value;
-    if (q_grid) window_grad_q<float, D><<<q_grid, 256, 0, st>>>(g);
+    if (q_grid) window_grad_q<float, D><<<dim3(q_grid, g.q_splits), 256, 0, st>>>(g);
     if (g.blocks) window_grad_kv<float, D><<<window_pieces(g), 256, 0, st>>>(g);
   };
   if (d == 128) go(std::integral_constant<int, 128>{});
@@ -450,6 +476,11 @@ hipError_t launch_window_grad_join(const WindowGradArgs& g, bool bf16, int d, hi
   const int split_blocks = g.parts > 1 ? g.blocks : g.sink_blocks;
   const unsigned grid = (unsigned)(g.f.w.B * g.f.w.Hkv * split_blocks * (g.block / (1024 / d)));
   return by_type(bf16, d, [&](auto t, auto dc) { window_grad_join<decltype(t), decltype(dc)::value><<<grid, 256, 0, st>>>(g); });
+}
+
+hipError_t launch_window_grad_q_join(const WindowGradArgs& g, bool bf16, int d, hipStream_t st) {
+  const long long rows = (long long)g.f.w.B * g.f.w.Hq * g.f.w.Lq, per = 1024 / d;
+  return by_type(bf16, d, [&](auto t, auto dc) { window_grad_q_join<decltype(t), decltype(dc)::value><<<(unsigned)((rows + per - 1) / per), 256, 0, st>>>(g); });
 }
 
 }  // namespace usv

@@ -198,7 +198,10 @@ __global__ __launch_bounds__(256, WPS) void window_grad_q_bf16(WindowGradArgs g)
     if (e + kRows <= keys.count && (e >= keys.head || e + kRows <= keys.head)) tile.load(to, ka, va, window_key(keys, e));
     else tile.load_rows(to, ka, va, [&](int r) { return (long long)window_key(keys, min(e + r, keys.count - 1)); });
   };
-  if (tiles > 0) request(0);
+  int t0 = 0, t1 = tiles;
+  if (g.q_splits > 1) t0 = (int)((long long)tiles * blockIdx.y / g.q_splits), t1 = (int)((long long)tiles * (blockIdx.y + 1) / g.q_splits);
+  t0 = __builtin_amdgcn_readfirstlane(t0), t1 = __builtin_amdgcn_readfirstlane(t1);
+  if (t0 < t1) request(t0);
 
   bf16x8 qf[2][D / 32], dof[2][D / 32];
   float nlse[2], delta[2];
@@ -224,7 +227,7 @@ __global__ __launch_bounds__(256, WPS) void window_grad_q_bf16(WindowGradArgs g)
       delta[nt] = sum_over_groups(sum);
       nlse[nt] = -a.lse[id] * kLog2e;
       range[nt] = window_range(a.w, seq.n, seq.first + some);
-      if (G == 0 && row == some)
+      if (G == 0 && row == some && blockIdx.y == 0)
         g.delta[id] = nlse[nt], g.delta[id + g.plane] = delta[nt], g.delta[id + 2 * g.plane] = __int_as_float(range[nt].lo), g.delta[id + 3 * g.plane] = __int_as_float(range[nt].hi);
     }
   }
@@ -243,7 +246,7 @@ __global__ __launch_bounds__(256, WPS) void window_grad_q_bf16(WindowGradArgs g)
     constexpr bool OPEN = decltype(open_c)::value;
     wait_vm<0>();
     __syncthreads();  // the tile is there; everybody is done with the other stage
-    if (t + 1 < tiles) request(t + 1);
+    if (t + 1 < t1) request(t + 1);
     const unsigned char* kt = smem + (t & 1) * T::STAGE;
     const unsigned char* vt = kt + T::TENSOR;
 #pragma unroll
@@ -285,15 +288,25 @@ __global__ __launch_bounds__(256, WPS) void window_grad_q_bf16(WindowGradArgs g)
       pin(dq);
     }
   };
-  for (int t = 0; t < tiles;) {
-    for (; t < tiles && window_tile_open(keys, t * kRows, kRows); ++t) step(std::true_type{}, t);
-    for (; t < tiles && !window_tile_open(keys, t * kRows, kRows); ++t) step(std::false_type{}, t);
+  for (int t = t0; t < t1;) {
+    for (; t < t1 && window_tile_open(keys, t * kRows, kRows); ++t) step(std::true_type{}, t);
+    for (; t < t1 && !window_tile_open(keys, t * kRows, kRows); ++t) step(std::false_type{}, t);
   }
 #pragma unroll
   for (int nt = 0; nt < 2; ++nt) {
     const int row = row0 + 16 * nt + c;
     if (row >= a.w.Lq) continue;
     const bool live = row >= keys.i0 && row < keys.i1;
+    if (g.q_splits > 1) {
+      const long long id = ((long long)slot.b * a.w.Hq + slot.h) * a.w.Lq + row;
+      float* part = g.dq_part + (blockIdx.y * g.plane + id) * D + 4 * G;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) {
+        const f32x4 x = quarter(dq[nt][dt >> 2], dt & 3);
+        store4<true>(part + 16 * dt, live ? make_float4(x[0], x[1], x[2], x[3]) : make_float4(0.f, 0.f, 0.f, 0.f), 0);
+      }
+      continue;
+    }
     uint16_t* dst = row_of(g.dq, g.sdq, slot.b, slot.h, row) + 4 * G;
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) {
@@ -476,7 +489,7 @@ hipError_t run(const WindowGradArgs& args, hipStream_t st) {
   window_slots(&g.f, kBlock128);
   g.plane = (long long)g.f.w.B * g.f.w.Hq * g.f.w.Lq;
   const unsigned q_grid = (unsigned)((g.f.w.Lq + kBlock128 - 1) / kBlock128 * g.f.w.B * g.f.w.Hq);
-  if (q_grid) window_grad_q_bf16<D, WPS><<<q_grid, 256, 0, st>>>(g);
+  if (q_grid) window_grad_q_bf16<D, WPS><<<dim3(q_grid, g.q_splits), 256, 0, st>>>(g);
   if (g.blocks) window_grad_kv_bf16<D, WPS><<<window_pieces(g), 256, 0, st>>>(g);
   return hipGetLastError();
 }

@@ -200,6 +200,39 @@ def test_long_windows_of_few_rows(usv, d):
                     close_lse(lse[0, h], f64(ls))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq, Hkv, Lq, Lk, left, right, sinks, chunk", [
+    (2, 1, 1500, 1500, 300, 0, 40, 1),    # lists of rows shared out, those of the sinks in more pieces
+    (1, 1, 70, 5000, 4300, 0, 10, 1),     # lists of keys shared out
+    (3, 1, 900, 2300, 2, 1, 1, 250),
+    (8, 2, 40, 3000, -1, 0, 0, 1),
+])
+def test_gradients_of_long_lists(usv, d, dtype, Hq, Hkv, Lq, Lk, left, right, sinks, chunk):
+    a = dict(left=left, right=right, sinks=sinks, chunk=chunk)
+    q, do = (normal((1, Hq, Lq, d), 300 + i, TYPES[dtype]).to(DEV) for i in range(2))
+    k, v = (normal((1, Hkv, Lk, d), 310 + i, TYPES[dtype]).to(DEV) for i in range(2))
+    out, lse = usv.window_attn(q, k, v, **a, return_lse=True)
+    dq, dk, dv = usv.window_attn_backward(q, k, v, out, lse, do, **a)
+    M = torch.from_numpy(wo.masks(1, Lq, Lk, left, right, sinks, chunk)[0]).to(DEV)
+    scale, G = d ** -0.5, Hq // Hkv
+    want = [torch.zeros((Hkv, Lk, d), dtype=torch.float64, device=DEV) for _ in range(6)]  # dk, dv, their magnitudes, terms of dk
+    for h in range(Hq):
+        Q, K, V, dO, O = (x.double() for x in (q[0, h], k[0, h // G], v[0, h // G], do[0, h], out[0, h]))
+        x = (Q @ K.T * scale).masked_fill(~M, -float("inf"))
+        P = torch.softmax(x, 1)
+        D = (dO * O).sum(1, keepdim=True)
+        dS = P * (dO @ V.T - D) * scale
+        T = P * (dO.abs() @ V.abs().T + (dO * O).abs().sum(1, keepdim=True)) * scale
+        close(dq[0, h], f64(dS @ K), f64(dS.abs() @ K.abs()), dtype, f"dq of head {h}", f64(T @ K.abs()))
+        for i, y in enumerate((dS.T @ Q, P.T @ dO, dS.abs().T @ Q.abs(), P.T @ dO.abs(), T.T @ Q.abs())):
+            want[i][h // G] += y
+    close(dk[0], f64(want[0]), f64(want[2]), dtype, "dk", f64(want[4]))
+    close(dv[0], f64(want[1]), f64(want[3]), dtype, "dv")
+    for x, y in zip((dq, dk, dv), usv.window_attn_backward(q, k, v, out, lse, do, **a)):
+        assert torch.equal(x, y)
+
+
 def test_empty_lengths(usv):
     q, k = torch.zeros((1, 2, 0, 64), device=DEV), torch.randn((1, 2, 5, 64), device=DEV)
     out, lse = usv.window_attn(q, k, k, -1, return_lse=True)
