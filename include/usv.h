@@ -577,7 +577,9 @@ size_t usv_window_backward_workspace_bytes(const usv_window* w);
 /* Gradients of usv_window_attn: with P = exp(scale q.k - lse), D = sum over the channels of dout * out,
  *   dS = P (dout.v - D),  dq = scale dS k,  dk = scale dS^T q,  dv = P^T dout,
  * dk and dv summed over the query heads that share a key head.
- * q, k, v, out, lse : as given to and written by usv_window_attn with the same `w` and scale (device, read only)
+ * q, k, v, out, lse : as given to and written by usv_window_attn with the same `w` and scale (device, read only); an out or lse of
+ *         other keys (of a part of them, or of more) is none: USV_BF16 takes from dS adding up to 0 over the keys of a row what the
+ *         rounding of `out` costs D
  * dout  : [B, q_heads, q_len, d] of w->dtype (device, read only); rows without a token may hold anything
  * dq, dk, dv : the shapes of q, k, v, of w->dtype (written); rows that see nothing or are seen by no query are 0
  * ws    : device scratch >= usv_window_backward_workspace_bytes(w); contents on return unspecified

@@ -63,9 +63,10 @@ def window_attn(Q, K, V, M, scale=None):
     return out, lse, mag
 
 
-def window_attn_backward(Q, K, V, out, dout, M, scale=None):
-    """dq, dk, dv for the given `out`; for each what relative errors of P and dS act on; and what those of dout.v and D act on."""
-    Q, K, V, out, dout = (np.asarray(x, dtype=np.float64) for x in (Q, K, V, out, dout))
+def window_attn_backward(Q, K, V, dout, M, scale=None):
+    """dq, dk, dv; for each what relative errors of P and dS act on; and what those of dout.v and D act on.  (In dq an error of a row's dS may
+    be taken off all its keys in proportion to P, since dS adds up to 0: it then acts on sum P |k| too.)"""
+    Q, K, V, dout = (np.asarray(x, dtype=np.float64) for x in (Q, K, V, dout))
     B, Hq, Lq, d = Q.shape
     G = Hq // K.shape[1]
     scale = 1.0 / math.sqrt(d) if scale is None else scale
@@ -77,13 +78,14 @@ def window_attn_backward(Q, K, V, out, dout, M, scale=None):
         for h in range(Hq):
             g = h // G
             P = _weights(Q[b, h], K[b, g], M[b], scale)[0][np.ix_(live, some)]
-            q, do, o, k, v = Q[b, h][live], dout[b, h][live], out[b, h][live], K[b, g][some], V[b, g][some]
+            q, do, k, v = Q[b, h][live], dout[b, h][live], K[b, g][some], V[b, g][some]
+            o = P @ v
             dS = P * (do @ v.T - (do * o).sum(1, keepdims=True)) * scale
             terms = P * (np.abs(do) @ np.abs(v).T + np.abs(do * o).sum(1, keepdims=True)) * scale  # sums of absolute products
             dq[b, h][live] = dS @ k
             dk[b, g][some] += dS.T @ q
             dv[b, g][some] += P.T @ do
-            mq[b, h][live] = np.abs(dS) @ np.abs(k)
+            mq[b, h][live] = np.abs(dS) @ np.abs(k) + np.abs(dS).sum(1, keepdims=True) * (P @ np.abs(k))
             mk[b, g][some] += np.abs(dS).T @ np.abs(q)
             eq[b, h][live] = terms @ np.abs(k)
             ek[b, g][some] += terms.T @ np.abs(q)

@@ -69,7 +69,7 @@ struct WindowGradArgs {
   int block, blocks, sink_blocks, sink_parts, parts;
   float* partial;  // dk, dv of the pieces: [slot][2][block][d]; a block in one piece has no slot
   Div by_heads, by_sink_parts, by_parts;
-  int q_splits;    // > 1: the key lists of the query rows are shared out too, dq of the pieces goes to dq_part [q_splits][rows][d] (fp32, unscaled)
+  int q_splits;    // fp32, > 1: the key lists of the query rows are shared out too, dq of the pieces goes to dq_part [q_splits][rows][d] (fp32, unscaled)
   float* dq_part;
 };
 
@@ -219,6 +219,6 @@ hipError_t launch_window_join(const WindowArgs& a, bool bf16, int d, hipStream_t
 hipError_t launch_window_grad_f32(const WindowGradArgs& a, int d, hipStream_t st);
 hipError_t launch_window_grad_bf16(const WindowGradArgs& a, int d, hipStream_t st);
 hipError_t launch_window_grad_join(const WindowGradArgs& a, bool bf16, int d, hipStream_t st);    // dk, dv
-hipError_t launch_window_grad_q_join(const WindowGradArgs& a, bool bf16, int d, hipStream_t st);  // dq
+hipError_t launch_window_grad_q_join(const WindowGradArgs& a, int d, hipStream_t st);  // dq, fp32
 
 }  // namespace usv

@@ -415,7 +415,7 @@ __global__ __launch_bounds__(256) void window_grad_join(WindowGradArgs g) {
 }
 
 // dq of a row = sum of its pieces, in their order.
-template <typename T, int D>
+template <int D>
 __global__ __launch_bounds__(256) void window_grad_q_join(WindowGradArgs g) {
   const WindowArgs& a = g.f;
   const long long rows = (long long)a.w.B * a.w.Hq * a.w.Lq;
@@ -429,7 +429,7 @@ __global__ __launch_bounds__(256) void window_grad_q_join(WindowGradArgs g) {
     sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
   }
   const int row = (int)(id % a.w.Lq), bh = (int)(id / a.w.Lq);
-  put4<T>(row_of<T>(g.dq, g.sdq, bh / a.w.Hq, bh % a.w.Hq, row) + ch, make_float4(sum.x * a.scale, sum.y * a.scale, sum.z * a.scale, sum.w * a.scale));
+  put4<float>(row_of<float>(g.dq, g.sdq, bh / a.w.Hq, bh % a.w.Hq, row) + ch, make_float4(sum.x * a.scale, sum.y * a.scale, sum.z * a.scale, sum.w * a.scale));
 }
 
 template <typename F>
@@ -478,9 +478,12 @@ hipError_t launch_window_grad_join(const WindowGradArgs& g, bool bf16, int d, hi
   return by_type(bf16, d, [&](auto t, auto dc) { window_grad_join<decltype(t), decltype(dc)::value><<<grid, 256, 0, st>>>(g); });
 }
 
-hipError_t launch_window_grad_q_join(const WindowGradArgs& g, bool bf16, int d, hipStream_t st) {
+hipError_t launch_window_grad_q_join(const WindowGradArgs& g, int d, hipStream_t st) {
   const long long rows = (long long)g.f.w.B * g.f.w.Hq * g.f.w.Lq, per = 1024 / d;
-  return by_type(bf16, d, [&](auto t, auto dc) { window_grad_q_join<decltype(t), decltype(dc)::value><<<(unsigned)((rows + per - 1) / per), 256, 0, st>>>(g); });
+  const unsigned grid = (unsigned)((rows + per - 1) / per);
+  if (d == 128) window_grad_q_join<128><<<grid, 256, 0, st>>>(g);
+  else window_grad_q_join<64><<<grid, 256, 0, st>>>(g);
+  return hipGetLastError();
 }
 
 }  // namespace usv

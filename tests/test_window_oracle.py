@@ -36,7 +36,7 @@ def test_values_and_gradients_against_torch(seed):
     K, V = rng.standard_normal((2, B, Hkv, L, d))
     M = wo.masks(B, L, L, [3, -1, 0, 2][seed], [0, 0, 1, -1][seed], seed % 3, [1, 1, 4, 5][seed], 0, [L, 9])
     out, lse, mag = wo.window_attn(Q, K, V, M)
-    (dq, dk, dv), _, _ = wo.window_attn_backward(Q, K, V, out, dO, M)
+    (dq, dk, dv), _, _ = wo.window_attn_backward(Q, K, V, dO, M)
     q, k, v = (torch.tensor(x, requires_grad=True) for x in (Q, K, V))
     kk, vv = (x.repeat_interleave(2, 1) for x in (k, v))
     Mt = torch.tensor(M)[:, None]
