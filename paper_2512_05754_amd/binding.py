@@ -232,7 +232,9 @@ def lib() -> ctypes.CDLL:
     L.usv_last_error.restype, L.usv_last_error.argtypes = ctypes.c_char_p, []
     if calls is not None:
         calls.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
-            L.usv_block_scores, L.usv_select_topk_ex, L.usv_attn_work_order, L.usv_block_sparse_attn, L.usv_block_sparse_attn_ordered)))
+            L.usv_block_scores, L.usv_select_topk_ex, L.usv_attn_work_order, L.usv_block_sparse_attn, L.usv_block_sparse_attn_ordered,
+            L.usv_window_workspace_bytes, L.usv_window_attn, L.usv_window_backward_workspace_bytes, L.usv_window_attn_backward,
+            L.usv_cache_write, L.usv_cache_read, L.usv_cache_attn_workspace_bytes, L.usv_cache_attn)))
     _lib, _calls = L, calls
     return L
 
@@ -784,6 +786,13 @@ def block_sparse_attn_raster(q, k, v, order, idx, cnt, scale=0.0, out=None, out_
     return (out, lse) if return_lse else out
 
 
+def _done(got):
+    """Results of the extension, or the status of a call that the library has refused."""
+    if type(got) is int:
+        _check(got)
+    return got
+
+
 def _rows(t: torch.Tensor, name: str, like: torch.Tensor, shape=None):
     """Pointer and element strides of a [B, heads, len, d] tensor with contiguous channels, of `like`'s type and device."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -830,14 +839,23 @@ def _scratch(t, name, nbytes, like):
     return t, (_dev(t, name) if t.numel() else None), t.numel() * t.element_size()
 
 
+def _int32(**values):
+    """The values as whole numbers of 32 bits (the argument structs would take the low bits of larger ones)."""
+    for name, x in values.items():
+        values[name] = int(x)
+        if not -(1 << 31) <= values[name] < 1 << 31:
+            raise ValueError(f"{name} ({x}) is beyond 32 bits")
+    return values.values()
+
+
 def _window(q, left, right, sinks, chunk, q_start, seq_lens, kv_heads, kv_len):
     if not isinstance(q, torch.Tensor) or not q.is_cuda:
         raise TypeError("q must be a GPU tensor (there is no CPU path)")
     if q.dim() != 4:
         raise ValueError("q must be [B, heads, len, d]")
     B, Hq, Lq, d = q.shape
-    w = UsvWindow(B, Hq, kv_heads, Lq, kv_len, d, _dt(q), int(left), int(right), int(sinks), int(chunk),
-                  USV_Q_AT_END if q_start is None else int(q_start))
+    w = UsvWindow(*_int32(batch=B, q_heads=Hq, kv_heads=kv_heads, q_len=Lq, kv_len=kv_len, head_dim=d), _dt(q),
+                  *_int32(left=left, right=right, sinks=sinks, chunk=chunk, q_start=USV_Q_AT_END if q_start is None else q_start))
     if seq_lens is not None:
         w.seq_lens = _vector(seq_lens, "seq_lens", (B,), torch.int32, q)
     return w
@@ -866,6 +884,10 @@ def window_attn(q, k, v, left, right=0, sinks=0, chunk=1, q_start=None, seq_lens
     (negative left or right: all).  q_start: position of query row 0; None: the queries are the newest tokens.  seq_lens: int32 [B],
     tokens of each sequence of a padded batch.  workspace: uint8 scratch of window_workspace_bytes(...); None: one is allocated where
     the call has a use for one."""
+    if _calls is not None:
+        got = _calls.window_attn(q, k, v, left, right, sinks, chunk, q_start, seq_lens, scale, out, lse, return_lse, workspace)
+        if got is not None:
+            return _done(got)
     w, qp, kp, vp_ = _window_of(q, k, v, left, right, sinks, chunk, q_start, seq_lens)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
@@ -887,6 +909,10 @@ def window_attn_backward(q, k, v, out, lse, dout, left, right=0, sinks=0, chunk=
     """usv_window_attn_backward: gradients (dq, dk, dv) of window_attn, from its inputs, its out and lse, and the gradient of out.
 
     workspace: uint8 scratch of window_workspace_bytes(..., backward=True); None: one is allocated."""
+    if _calls is not None:
+        got = _calls.window_attn_backward(q, k, v, out, lse, dout, left, right, sinks, chunk, q_start, seq_lens, scale, dq, dk, dv, workspace)
+        if got is not None:
+            return _done(got)
     w, qp, kp, vp_ = _window_of(q, k, v, left, right, sinks, chunk, q_start, seq_lens)
     op, w.out = _rows(out, "out", q, q.shape)
     lp = _vector(lse, "lse", q.shape[:3], torch.float32, q)
@@ -916,7 +942,7 @@ def window_workspace_bytes(q, k, left, right=0, sinks=0, chunk=1, backward=False
 
 def cache_empty(pages, kv_heads, page_size, head_dim, bits=4, device="cuda:0"):
     """A cache of `pages` pages of page_size positions: uint8 [pages, kv_heads, bytes], uninitialised."""
-    c = UsvCache(1, int(kv_heads), int(head_dim), int(bits), int(page_size), int(pages), 1, None)
+    c = UsvCache(1, *_int32(kv_heads=kv_heads, head_dim=head_dim, bits=bits, page_size=page_size, pages=pages), 1, None)
     n = int(lib().usv_cache_bytes(ctypes.byref(c)))
     if n == 0:
         raise ValueError(lib().usv_last_error().decode())
@@ -934,12 +960,14 @@ def _cache(cache, page_table, head_dim, bits):
     per = 2 * (head_dim * int(bits) // 8 + head_dim // 32)  # bytes of a position: codes and scales of K and V
     if per <= 0 or cache.shape[2] % per != 0:
         raise ValueError(f"a page of {cache.shape[2]} bytes does not hold rows of {head_dim} channels in {bits} bits")
-    return UsvCache(page_table.shape[0], cache.shape[1], head_dim, int(bits), cache.shape[2] // per, cache.shape[0], page_table.shape[1], tp), p
+    return UsvCache(*_int32(batch=page_table.shape[0], kv_heads=cache.shape[1], head_dim=head_dim, bits=bits, page_size=cache.shape[2] // per,
+                            pages=cache.shape[0], table_pages=page_table.shape[1]), tp), p
 
 
 def _cache_rows(cache, k, v, page_table, starts, counts, bits):
     c, p = _cache(cache, page_table, k.shape[3], bits)
     B, H, n, d = k.shape
+    _int32(rows=n)
     if B != c.batch or H != c.kv_heads:
         raise ValueError(f"k must be [{c.batch}, {c.kv_heads}, rows, d], got {list(k.shape)}")
     if k.device != cache.device:
@@ -954,6 +982,10 @@ def _cache_rows(cache, k, v, page_table, starts, counts, bits):
 def cache_write(cache, k, v, page_table, starts, bits=4, counts=None):
     """usv_cache_write: quantises rows k, v [B, Hkv, n, d] (bf16 or fp32, any strides with contiguous channels) into the cache, row i of
     sequence b at position starts[b] + i.  page_table int32 [B, pages of a sequence]; starts, counts int32 [B] (counts: rows that count)."""
+    if _calls is not None:
+        got = _calls.cache_write(cache, k, v, page_table, starts, bits, counts)
+        if got is not None:
+            return _done(got)
     for name, t in (("k", k), ("v", v)):
         if not isinstance(t, torch.Tensor) or not t.is_cuda:
             raise TypeError(f"{name} must be a GPU tensor (there is no CPU path)")
@@ -967,6 +999,10 @@ def cache_write(cache, k, v, page_table, starts, bits=4, counts=None):
 
 def cache_read(cache, page_table, starts, rows, head_dim=128, bits=4, counts=None, dtype=torch.bfloat16, k=None, v=None):
     """usv_cache_read: the values held at positions starts[b] + i, i < rows -> k, v [B, Hkv, rows, d] of dtype (or into the given k, v)."""
+    if _calls is not None:
+        got = _calls.cache_read(cache, page_table, starts, rows, head_dim, bits, counts, dtype, k, v)
+        if got is not None:
+            return _done(got)
     if not isinstance(cache, torch.Tensor) or cache.dim() != 3 or not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
         raise ValueError("cache must be [pages, kv_heads, bytes] and page_table [B, pages of a sequence]")
     shape = (page_table.shape[0], cache.shape[1], int(rows), int(head_dim))
@@ -999,6 +1035,10 @@ def cache_attn(q, cache, page_table, seq_lens, left=-1, right=0, sinks=0, chunk=
 
     seq_lens int32 [B]: tokens of each sequence in the cache, the queries' own included; left, right, sinks, chunk as window_attn.
     workspace: uint8 scratch of cache_attn_workspace_bytes(...); None: one is allocated where the call has a use for one."""
+    if _calls is not None:
+        got = _calls.cache_attn(q, cache, page_table, seq_lens, left, right, sinks, chunk, bits, scale, out, lse, return_lse, workspace)
+        if got is not None:
+            return _done(got)
     c, p, w = _cache_window(q, cache, page_table, seq_lens, left, right, sinks, chunk, bits)
     qp, w.q = _rows(q, "q", q)
     if out is None:

@@ -1,16 +1,23 @@
 // Marshalling of the calls that a small step is made of, as a CPython extension: the three stages and the work order on tensors that
-// are all there already.  A call of a few microseconds of kernels is bound by its host side, and reading a tensor's shape, type and
+// are all there already, and windowed attention and the cache.  A call of a few microseconds of kernels is bound by its host side, and reading a tensor's shape, type and
 // address costs Python about 0.4 us a tensor and the foreign-function call another 1.5 us (three stages on 1024 tokens, fp32: 21.5 -> 17.2 us with the kernels of 17 us that they launch; the first pass on new inputs 57 -> 41).
 //
 // Every function takes what the binding's function of that name was given, checks what it checks, calls the library and returns its
 // status; or it returns None, having done nothing, for whatever it does not know: the binding then goes its own way, which also says
-// what is wrong with an argument.  No tensor is kept, allocated or changed, and no exception of torch's leaves a function.
+// what is wrong with an argument.  No tensor is kept, and no exception of torch's leaves a function.  Windowed attention and the cache
+// also make the results and the scratch that they were not given, and return the results in place of a status of 0.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/ops/empty.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <algorithm>
+#include <cstring>
 
 #include "usv.h"
 
@@ -22,6 +29,14 @@ struct Table {
   decltype(&usv_attn_work_order) attn_work_order;
   decltype(&usv_block_sparse_attn) block_sparse_attn;
   decltype(&usv_block_sparse_attn_ordered) block_sparse_attn_ordered;
+  decltype(&usv_window_workspace_bytes) window_workspace_bytes;
+  decltype(&usv_window_attn) window_attn;
+  decltype(&usv_window_backward_workspace_bytes) window_backward_workspace_bytes;
+  decltype(&usv_window_attn_backward) window_attn_backward;
+  decltype(&usv_cache_write) cache_write;
+  decltype(&usv_cache_read) cache_read;
+  decltype(&usv_cache_attn_workspace_bytes) cache_attn_workspace_bytes;
+  decltype(&usv_cache_attn) cache_attn;
 } table;  // of the library the binding has loaded
 
 // A plain tensor in GPU memory (no subclass, which may stand for something else; no wrapper without storage of its own).
@@ -168,24 +183,283 @@ PyObject* block_sparse_attn(PyObject* const* a, Py_ssize_t n) {
   return call([&] { return table.block_sparse_attn_ordered(qp, kp, vp, &s, ip, cp, kmax, wp, scale, odt, op, lp, st); });
 }
 
-// (the addresses of the five functions above, in the table's order)
+// ---- windowed attention and the cache
+
+// A plain strided tensor on the current device (whose current stream the launch goes to).
+bool strided(PyObject* o, const at::Tensor** t) {
+  if (!THPVariable_CheckExact(o)) return false;
+  const at::Tensor& x = THPVariable_Unpack(o);
+  if (!x.defined() || !x.is_cuda() || x.layout() != at::kStrided || !x.has_storage() || x.get_device() != c10::hip::current_device()) return false;
+  *t = &x;
+  return true;
+}
+// ... contiguous, of this type and shape
+bool vector(PyObject* o, at::ScalarType type, at::IntArrayRef shape, const at::Tensor** t) {
+  return strided(o, t) && (*t)->is_contiguous() && (*t)->scalar_type() == type && (*t)->sizes() == shape;
+}
+bool dtype_of(at::ScalarType t, int32_t* dtype) {
+  if (t != at::kBFloat16 && t != at::kFloat) return false;
+  *dtype = t == at::kFloat ? USV_F32 : USV_BF16;
+  return true;
+}
+// Address and strides of rows [B, heads, len, d] with contiguous channels.  (A dimension of one entry has a stride that says nothing.)
+bool rows_of(const at::Tensor& x, void** p, usv_strides* st) {
+  if (x.dim() != 4) return false;
+  const auto n = x.sizes(), s = x.strides();
+  for (int64_t e : n)
+    if (!fits(e)) return false;
+  *p = nullptr, *st = usv_strides{0, 0, 0};
+  if (x.numel() == 0) return true;
+  if (s[3] != 1 || (n[2] > 1 && s[2] == 0)) return false;
+  *p = x.data_ptr();
+  *st = usv_strides{n[0] > 1 ? s[0] : n[1] * n[2] * n[3], n[1] > 1 ? s[1] : n[2] * n[3], n[2] > 1 ? s[2] : n[3]};
+  return true;
+}
+bool rows_of(PyObject* o, const at::Tensor& like, at::IntArrayRef shape, void** p, usv_strides* st) {
+  const at::Tensor* t;
+  return strided(o, &t) && t->scalar_type() == like.scalar_type() && t->sizes() == shape && rows_of(*t, p, st);
+}
+
+// A result: the caller's tensor, or a new one.
+struct Result {
+  PyObject* object = nullptr;
+  ~Result() { Py_XDECREF(object); }
+  bool rows(PyObject* o, at::IntArrayRef shape, const at::TensorOptions& like, const at::Tensor& type, void** p, usv_strides* st) {
+    if (o != Py_None) {
+      Py_INCREF(object = o);
+      return rows_of(o, type, shape, p, st);
+    }
+    const at::Tensor t = at::empty(shape, like);
+    return rows_of(t, p, st) && (object = THPVariable_Wrap(t));
+  }
+  bool lse(PyObject* o, bool wanted, const at::Tensor& q, float** p) {
+    *p = nullptr;
+    const auto shape = q.sizes().slice(0, 3);
+    if (o != Py_None) {
+      const at::Tensor* t;
+      Py_INCREF(object = o);
+      if (!vector(o, at::kFloat, shape, &t)) return false;
+      *p = static_cast<float*>(t->data_ptr());
+    } else if (wanted) {
+      const at::Tensor t = at::empty(shape, q.options().dtype(at::kFloat));
+      *p = static_cast<float*>(t.data_ptr());
+      return (object = THPVariable_Wrap(t));
+    }
+    return true;
+  }
+  PyObject* give() {
+    PyObject* o = object;
+    object = nullptr;
+    return o;
+  }
+};
+// Scratch: the caller's, or a new one of `need` bytes; it may go when its launch has been enqueued.
+struct Scratch {
+  at::Tensor made;
+  void* p = nullptr;
+  size_t bytes = 0;
+  bool take(PyObject* o, const at::Tensor& like, size_t need) {
+    const at::Tensor* t = &made;
+    if (o != Py_None) {
+      if (!strided(o, &t) || !t->is_contiguous()) return false;
+    } else if (need) made = at::empty({(int64_t)need}, like.options().dtype(at::kByte));
+    else return true;
+    bytes = t->nbytes();
+    p = bytes ? t->data_ptr() : nullptr;
+    return true;
+  }
+};
+// `out`, or (out, lse); a status that is not 0
+PyObject* answer(PyObject* status, Result& out, Result* lse) {
+  if (!status || PyLong_AsLong(status) != 0) return status;
+  Py_DECREF(status);
+  if (!lse) return out.give();
+  return Py_BuildValue("(NN)", out.give(), lse->give());
+}
+
+// a: left, right, sinks, chunk
+bool window_of(const at::Tensor& q, PyObject* const* a, PyObject* q_start, PyObject* seq_lens, int64_t kv_heads, int64_t kv_len, usv_window* w) {
+  if (q.dim() != 4 || !dtype_of(q.scalar_type(), &w->dtype) || !fits(kv_heads) || !fits(kv_len)) return false;
+  if (!whole(a[0], &w->left) || !whole(a[1], &w->right) || !whole(a[2], &w->sinks) || !whole(a[3], &w->chunk)) return false;
+  const auto n = q.sizes();
+  for (int64_t e : n)
+    if (!fits(e)) return false;
+  w->batch = (int32_t)n[0], w->q_heads = (int32_t)n[1], w->q_len = (int32_t)n[2], w->head_dim = (int32_t)n[3];
+  w->kv_heads = (int32_t)kv_heads, w->kv_len = (int32_t)kv_len;
+  w->q_start = USV_Q_AT_END;
+  if (q_start != Py_None && !whole(q_start, &w->q_start)) return false;
+  w->seq_lens = nullptr;
+  if (seq_lens != Py_None) {
+    const at::Tensor* t;
+    if (!vector(seq_lens, at::kInt, n.slice(0, 1), &t)) return false;
+    w->seq_lens = static_cast<const int32_t*>(t->data_ptr());
+  }
+  return true;
+}
+bool window_tensors(PyObject* const* a, const at::Tensor** q, const at::Tensor** k, void** p, usv_window* w) {  // a: q, k, v
+  if (!strided(a[0], q) || !strided(a[1], k) || (*q)->dim() != 4 || (*k)->dim() != 4 || (*q)->scalar_type() != (*k)->scalar_type()) return false;
+  const auto n = (*q)->sizes(), m = (*k)->sizes();
+  return m[0] == n[0] && m[3] == n[3] && rows_of(**q, &p[0], &w->q) && rows_of(**k, &p[1], &w->k) && rows_of(a[2], **q, m, &p[2], &w->v);
+}
+bool flag(PyObject* o) { return o == Py_True || o == Py_False; }
+
+// (q, k, v, left, right, sinks, chunk, q_start, seq_lens, scale, out, lse, return_lse, workspace)
+PyObject* window_attn(PyObject* const* a, Py_ssize_t n) {
+  const at::Tensor *q, *k;
+  usv_window w = {};
+  void *p[3], *op;
+  float* lp;
+  Result out, lse;
+  Scratch ws;
+  if (n != 14 || !table.window_attn || !PyFloat_CheckExact(a[9]) || !flag(a[12]) || !window_tensors(a, &q, &k, p, &w)) return nullptr;
+  if (!window_of(*q, a + 3, a[7], a[8], k->size(1), k->size(2), &w)) return nullptr;
+  if (!out.rows(a[10], q->sizes(), q->options(), *q, &op, &w.out) || !lse.lse(a[11], a[12] == Py_True, *q, &lp)) return nullptr;
+  if (!ws.take(a[13], *q, a[13] == Py_None ? table.window_workspace_bytes(&w) : 0)) return nullptr;
+  const float scale = (float)PyFloat_AS_DOUBLE(a[9]);
+  void* st = stream();
+  return answer(call([&] { return table.window_attn(p[0], p[1], p[2], &w, scale, op, lp, ws.p, ws.bytes, st); }), out, a[12] == Py_True ? &lse : nullptr);
+}
+
+// (q, k, v, out, lse, dout, left, right, sinks, chunk, q_start, seq_lens, scale, dq, dk, dv, workspace)
+PyObject* window_attn_backward(PyObject* const* a, Py_ssize_t n) {
+  const at::Tensor *q, *k, *lse;
+  usv_window w = {};
+  usv_window_grads g = {};
+  void *p[3], *op, *dop, *gp[3];
+  Result dq, dk, dv;
+  Scratch ws;
+  if (n != 17 || !table.window_attn_backward || !PyFloat_CheckExact(a[12]) || !window_tensors(a, &q, &k, p, &w)) return nullptr;
+  if (!window_of(*q, a + 6, a[10], a[11], k->size(1), k->size(2), &w)) return nullptr;
+  if (!rows_of(a[3], *q, q->sizes(), &op, &w.out) || !vector(a[4], at::kFloat, q->sizes().slice(0, 3), &lse) || !rows_of(a[5], *q, q->sizes(), &dop, &g.dout))
+    return nullptr;
+  if (!dq.rows(a[13], q->sizes(), q->options(), *q, &gp[0], &g.dq) || !dk.rows(a[14], k->sizes(), q->options(), *q, &gp[1], &g.dk) ||
+      !dv.rows(a[15], k->sizes(), q->options(), *q, &gp[2], &g.dv))
+    return nullptr;
+  if (!ws.take(a[16], *q, a[16] == Py_None ? std::max<size_t>(table.window_backward_workspace_bytes(&w), 16) : 0)) return nullptr;
+  const float scale = (float)PyFloat_AS_DOUBLE(a[12]);
+  const float* lp = lse->numel() ? static_cast<const float*>(lse->data_ptr()) : nullptr;
+  void* st = stream();
+  PyObject* status = call([&] { return table.window_attn_backward(p[0], p[1], p[2], op, lp, dop, &w, &g, scale, gp[0], gp[1], gp[2], ws.p, ws.bytes, st); });
+  if (!status || PyLong_AsLong(status) != 0) return status;
+  Py_DECREF(status);
+  return Py_BuildValue("(NNN)", dq.give(), dk.give(), dv.give());
+}
+
+bool cache_of(PyObject* buffer, PyObject* page_table, int64_t d, PyObject* bits, usv_cache* c, void** p) {
+  const at::Tensor *x, *pages;
+  if (!strided(buffer, &x) || !x->is_contiguous() || x->scalar_type() != at::kByte || x->dim() != 3) return false;
+  if (!strided(page_table, &pages) || !pages->is_contiguous() || pages->scalar_type() != at::kInt || pages->dim() != 2) return false;
+  if (!whole(bits, &c->bits) || c->bits < 1 || c->bits > 32 || !fits(d)) return false;
+  const int64_t per = 2 * (d * c->bits / 8 + d / 32);  // bytes of a position: codes and scales of K and V
+  if (per <= 0 || x->size(2) % per != 0) return false;
+  const int64_t v[] = {pages->size(0), x->size(1), x->size(2) / per, x->size(0), pages->size(1)};
+  for (int64_t e : v)
+    if (!fits(e)) return false;
+  c->batch = (int32_t)v[0], c->kv_heads = (int32_t)v[1], c->page_size = (int32_t)v[2], c->pages = (int32_t)v[3], c->table_pages = (int32_t)v[4];
+  c->head_dim = (int32_t)d;
+  c->page_table = static_cast<const int32_t*>(pages->data_ptr());
+  *p = x->data_ptr();
+  return true;
+}
+bool counts_of(PyObject* starts, PyObject* counts, int64_t B, const int32_t** sp, const int32_t** np) {
+  const at::Tensor *s, *n;
+  if (!vector(starts, at::kInt, B, &s)) return false;
+  *sp = static_cast<const int32_t*>(s->data_ptr()), *np = nullptr;
+  if (counts == Py_None) return true;
+  if (!vector(counts, at::kInt, B, &n)) return false;
+  *np = static_cast<const int32_t*>(n->data_ptr());
+  return true;
+}
+
+// (cache, k, v, page_table, starts, bits, counts)
+PyObject* cache_write(PyObject* const* a, Py_ssize_t n) {
+  const at::Tensor* k;
+  usv_cache c = {};
+  usv_strides ks, vs;
+  void *p, *kp, *vp;
+  const int32_t *sp, *np;
+  int32_t dtype;
+  if (n != 7 || !table.cache_write || !strided(a[1], &k) || !dtype_of(k->scalar_type(), &dtype) || !rows_of(*k, &kp, &ks)) return nullptr;
+  if (!rows_of(a[2], *k, k->sizes(), &vp, &vs) || !cache_of(a[0], a[3], k->size(3), a[5], &c, &p)) return nullptr;
+  if (k->size(0) != c.batch || k->size(1) != c.kv_heads || !counts_of(a[4], a[6], c.batch, &sp, &np)) return nullptr;
+  const int32_t rows = (int32_t)k->size(2);
+  void* st = stream();
+  PyObject* status = call([&] { return table.cache_write(p, &c, kp, vp, dtype, rows, &ks, &vs, sp, np, st); });
+  if (!status || PyLong_AsLong(status) != 0) return status;
+  Py_DECREF(status);
+  Py_INCREF(a[0]);
+  return a[0];
+}
+
+// (cache, page_table, starts, rows, head_dim, bits, counts, dtype, k, v)
+PyObject* cache_read(PyObject* const* a, Py_ssize_t n) {
+  const at::Tensor *x, *given = nullptr;
+  usv_cache c = {};
+  usv_strides ks, vs;
+  void *p, *kp, *vp;
+  const int32_t *sp, *np;
+  int32_t dtype, rows, d;
+  Result k, v;
+  if (n != 10 || !table.cache_read || !whole(a[3], &rows) || rows < 0 || !whole(a[4], &d) || d < 0 || !THPDtype_Check(a[7])) return nullptr;
+  if (!cache_of(a[0], a[1], d, a[5], &c, &p) || !counts_of(a[2], a[6], c.batch, &sp, &np) || !strided(a[0], &x)) return nullptr;
+  at::ScalarType type = reinterpret_cast<THPDtype*>(a[7])->scalar_type;
+  for (PyObject* o : {a[8], a[9]})
+    if (o != Py_None) {
+      if (!strided(o, &given)) return nullptr;
+      type = given->scalar_type();
+    }
+  if (!dtype_of(type, &dtype)) return nullptr;
+  const int64_t shape[] = {c.batch, c.kv_heads, rows, d};
+  const auto like = x->options().dtype(type);
+  const at::Tensor& as = given ? *given : *x;
+  if (!k.rows(a[8], shape, like, as, &kp, &ks) || !v.rows(a[9], shape, like, as, &vp, &vs)) return nullptr;
+  void* st = stream();
+  return answer(call([&] { return table.cache_read(p, &c, kp, vp, dtype, rows, &ks, &vs, sp, np, st); }), k, &v);
+}
+
+// (q, cache, page_table, seq_lens, left, right, sinks, chunk, bits, scale, out, lse, return_lse, workspace)
+PyObject* cache_attn(PyObject* const* a, Py_ssize_t n) {
+  const at::Tensor* q;
+  usv_window w = {};
+  usv_cache c = {};
+  void *p, *qp, *op;
+  float* lp;
+  Result out, lse;
+  Scratch ws;
+  if (n != 14 || !table.cache_attn || !PyFloat_CheckExact(a[9]) || !flag(a[12]) || !strided(a[0], &q) || !rows_of(*q, &qp, &w.q)) return nullptr;
+  if (!cache_of(a[1], a[2], q->size(3), a[8], &c, &p) || a[3] == Py_None) return nullptr;
+  if (!window_of(*q, a + 4, Py_None, a[3], c.kv_heads, (int64_t)c.table_pages * c.page_size, &w)) return nullptr;
+  if (!out.rows(a[10], q->sizes(), q->options(), *q, &op, &w.out) || !lse.lse(a[11], a[12] == Py_True, *q, &lp)) return nullptr;
+  if (!ws.take(a[13], *q, a[13] == Py_None ? table.cache_attn_workspace_bytes(&c, &w) : 0)) return nullptr;
+  const float scale = (float)PyFloat_AS_DOUBLE(a[9]);
+  void* st = stream();
+  return answer(call([&] { return table.cache_attn(qp, p, &c, &w, scale, op, lp, ws.p, ws.bytes, st); }), out, a[12] == Py_True ? &lse : nullptr);
+}
+
+// (the addresses of the functions above, in the table's order)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void* p[5];
-  if (n != 5) return PyErr_Format(PyExc_TypeError, "five addresses");
-  for (int i = 0; i < 5; ++i) {
+  constexpr int N = sizeof(Table) / sizeof(void*);
+  void* p[N];
+  if (n != N) return PyErr_Format(PyExc_TypeError, "%d addresses", N);
+  for (int i = 0; i < N; ++i) {
     p[i] = PyLong_AsVoidPtr(a[i]);
     if (PyErr_Occurred()) return nullptr;
   }
-  table = Table{reinterpret_cast<decltype(table.block_scores)>(p[0]), reinterpret_cast<decltype(table.select_topk_ex)>(p[1]),
-                reinterpret_cast<decltype(table.attn_work_order)>(p[2]), reinterpret_cast<decltype(table.block_sparse_attn)>(p[3]),
-                reinterpret_cast<decltype(table.block_sparse_attn_ordered)>(p[4])};
+  static_assert(sizeof(table) == sizeof(p), "a table of addresses");
+  std::memcpy(&table, p, sizeof(p));
   Py_RETURN_NONE;
 }
 
 #define USV_METHOD(name, f) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {USV_METHOD("block_scores", guarded<block_scores>), USV_METHOD("select_topk", guarded<select_topk>),
                          USV_METHOD("attn_work_order", guarded<attn_work_order>),
-                         USV_METHOD("block_sparse_attn", guarded<block_sparse_attn>), USV_METHOD("bind", bind),
+                         USV_METHOD("block_sparse_attn", guarded<block_sparse_attn>),
+                         USV_METHOD("window_attn", guarded<window_attn>),
+                         USV_METHOD("window_attn_backward", guarded<window_attn_backward>),
+                         USV_METHOD("cache_write", guarded<cache_write>),
+                         USV_METHOD("cache_read", guarded<cache_read>),
+                         USV_METHOD("cache_attn", guarded<cache_attn>),
+                         USV_METHOD("bind", bind),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
