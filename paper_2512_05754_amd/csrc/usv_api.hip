@@ -220,7 +220,7 @@ void window_grad_plan(usv::WindowGradArgs* g, int block, int rows_per_tile, int 
   const long long longest = tiles(reach), sink_list = tiles(s.Lq);
   const long long all = heads * (g->sink_blocks * sink_list + (g->blocks - g->sink_blocks) * longest);
   long long piece = (all + slots - 1) / slots;
-  if (piece < 8) piece = 8;
+  if (piece < 2) piece = 2;  // (with 2 / 8: 3 x 20 heads of 89 rows 36 / 46 us, 8 heads of 130 rows 36 / 51, 2 x 2 of 500 in fp32 96 / 169; of 3 rows 36 / 33)
   auto parts = [&](long long list) { return list > 2 * piece ? (int)((list + piece - 1) / piece) : 1; };
   g->sink_parts = parts(sink_list);
   g->parts = parts(longest);
