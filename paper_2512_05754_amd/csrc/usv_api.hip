@@ -191,8 +191,8 @@ int window_pieces_of(const usv::WindowShape& s, int rows, long long slots, int l
 int window_splits(const usv::WindowShape& s, int d, bool bf16) {
   return bf16 ? window_pieces_of(s, usv::kWindowRows, d == 128 ? 1024 : 1536, 512) : window_pieces_of(s, usv::kWindowRows, 768, 256);
 }
-int window_grad_splits(const usv::WindowShape& s, bool bf16) {
-  return bf16 ? 1 : window_pieces_of(s, usv::kWindowRows, 512, 256);  // bf16: a piece would leave two rows and two sums
+int window_grad_splits(const usv::WindowShape& s, int d, bool bf16) {
+  return bf16 ? window_pieces_of(s, 128, d == 128 ? 512 : 768, 512) : window_pieces_of(s, usv::kWindowRows, 512, 256);
 }
 size_t window_part_bytes(const usv::WindowShape& s, int d, int splits) {
   return splits > 1 ? (size_t)splits * s.B * s.Hq * s.Lq * (d + 4) * sizeof(float) : 0;  // (d + 1, kept aligned)
@@ -232,7 +232,9 @@ size_t window_partial_bytes(const usv::WindowGradArgs& g, int d) {
   const size_t slots = heads * ((g.sink_parts > 1 ? (size_t)g.sink_blocks * g.sink_parts : 0) + (g.parts > 1 ? (size_t)(g.blocks - g.sink_blocks) * g.parts : 0));
   return slots * 2 * g.block * d * sizeof(float);
 }
-size_t window_dq_bytes(const usv::WindowShape& s, int d, int splits) { return splits > 1 ? (size_t)splits * s.B * s.Hq * s.Lq * d * sizeof(float) : 0; }
+size_t window_dq_bytes(const usv::WindowShape& s, int d, int splits, bool bf16) {
+  return splits > 1 ? (size_t)splits * s.B * s.Hq * s.Lq * (bf16 ? usv::window_dq_record(d) : d) * sizeof(float) : 0;
+}
 void window_grad_plan_for(usv::WindowGradArgs* g, const usv_window* w) {  // (workgroups: what the chip runs together)
   if (w->dtype == USV_BF16) window_grad_plan(g, 128, 64, w->head_dim == 128 ? 512 : 768);
   else window_grad_plan(g, 64, 32, w->head_dim == 128 ? 512 : 768);
@@ -861,7 +863,7 @@ size_t usv_window_backward_workspace_bytes(const usv_window* w) {
   window_grad_plan_for(&g, w);
   const bool bf16 = w->dtype == USV_BF16;
   const size_t n = window_delta_bytes(g.f.w, bf16) + window_partial_bytes(g, w->head_dim) +
-                   window_dq_bytes(g.f.w, w->head_dim, window_grad_splits(g.f.w, bf16));
+                   window_dq_bytes(g.f.w, w->head_dim, window_grad_splits(g.f.w, w->head_dim, bf16), bf16);
   return n ? n : 16;
 }
 
@@ -899,8 +901,8 @@ usv_status usv_window_attn_backward(const void* q, const void* k, const void* v,
   if (!(scale <= 0.f) && !std::isfinite(scale)) return fail(USV_ERR_INVALID_ARG, "scale must be finite");
   window_grad_plan_for(&g, w);
   USV_TRY(check_ptr(ws, "ws"));
-  g.q_splits = window_grad_splits(a.w, bf16);
-  const size_t need = window_delta_bytes(a.w, bf16) + window_partial_bytes(g, d) + window_dq_bytes(a.w, d, g.q_splits);
+  g.q_splits = window_grad_splits(a.w, d, bf16);
+  const size_t need = window_delta_bytes(a.w, bf16) + window_partial_bytes(g, d) + window_dq_bytes(a.w, d, g.q_splits, bf16);
   if (ws_bytes < need) return fail(USV_ERR_WORKSPACE, "ws holds %zu bytes, %zu are needed", ws_bytes, need);
   a.q = q, a.k = k, a.v = v, a.out = const_cast<void*>(out), a.lse = const_cast<float*>(lse);
   a.scale = scale > 0.f ? scale : 1.f / std::sqrt((float)d);
@@ -911,7 +913,6 @@ usv_status usv_window_attn_backward(const void* q, const void* k, const void* v,
   g.dq_part = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(g.partial) + window_partial_bytes(g, d));
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e = bf16 ? usv::launch_window_grad_bf16(g, d, st) : usv::launch_window_grad_f32(g, d, st);
-  if (e == hipSuccess && g.q_splits > 1) e = usv::launch_window_grad_q_join(g, d, st);
   if (e == hipSuccess && window_partial_bytes(g, d)) e = usv::launch_window_grad_join(g, bf16, d, st);
   return hip_result(e, "usv_window_attn_backward");
 }

@@ -58,6 +58,8 @@ inline void window_slots(WindowArgs* a, int rows) {
   a->by_items = div_by((a->w.Lq + rows - 1) / rows * a->w.group), a->by_rest = div_by(a->w.B * a->w.Hkv % kNumXcd);
 }
 
+inline constexpr int window_dq_record(int d) { return 2 * d + 4; }  // of a piece of a row, bf16: dq, sum P k, {sum dS, sum of the rounded dS, -, -}
+
 struct WindowGradArgs {
   WindowArgs f;  // q, k, v, out, lse as the forward pass left them
   const void* dout;
@@ -69,7 +71,9 @@ struct WindowGradArgs {
   int block, blocks, sink_blocks, sink_parts, parts;
   float* partial;  // dk, dv of the pieces: [slot][2][block][d]; a block in one piece has no slot
   Div by_heads, by_sink_parts, by_parts;
-  int q_splits;    // fp32, > 1: the key lists of the query rows are shared out too, dq of the pieces goes to dq_part [q_splits][rows][d] (fp32, unscaled)
+  // > 1: the key lists of the query rows are shared out too; what the pieces have goes to dq_part [q_splits][rows] (fp32): dq, unscaled, and in bf16
+  // sum P k and the two sums of dS behind it
+  int q_splits;
   float* dq_part;
 };
 
@@ -219,6 +223,6 @@ hipError_t launch_window_join(const WindowArgs& a, bool bf16, int d, hipStream_t
 hipError_t launch_window_grad_f32(const WindowGradArgs& a, int d, hipStream_t st);
 hipError_t launch_window_grad_bf16(const WindowGradArgs& a, int d, hipStream_t st);
 hipError_t launch_window_grad_join(const WindowGradArgs& a, bool bf16, int d, hipStream_t st);    // dk, dv
-hipError_t launch_window_grad_q_join(const WindowGradArgs& a, int d, hipStream_t st);  // dq, fp32
+hipError_t launch_window_grad_q_join(const WindowGradArgs& a, bool bf16, int d, hipStream_t st);  // dq; in bf16 also D
 
 }  // namespace usv

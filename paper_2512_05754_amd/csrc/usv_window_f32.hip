@@ -414,22 +414,30 @@ __global__ __launch_bounds__(256) void window_grad_join(WindowGradArgs g) {
   put4<T>(row_of<T>(g.dv, g.sdv, b, h, key) + ch, dv);
 }
 
-// dq of a row = sum of its pieces, in their order.
-template <int D>
+// dq of a row = sum of its pieces, in their order.  (bf16: what the kernel of the query rows does with them at its end)
+template <typename T, int D>
 __global__ __launch_bounds__(256) void window_grad_q_join(WindowGradArgs g) {
   const WindowArgs& a = g.f;
   const long long rows = (long long)a.w.B * a.w.Hq * a.w.Lq;
   const long long id = (long long)blockIdx.x * (1024 / D) + threadIdx.x / (D / 4);
   if (id >= rows) return;
   const int ch = 4 * (threadIdx.x % (D / 4));
-  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  constexpr bool BF16 = sizeof(T) == 2;
+  constexpr int REC = BF16 ? window_dq_record(D) : D;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f), pk = sum, ds = sum;
+  auto add = [](float4& s, const float4& x) { s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w; };
 #pragma unroll 4
   for (int s = 0; s < g.q_splits; ++s) {
-    const float4 x = load4(g.dq_part + (s * rows + id) * D + ch);
-    sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
+    const float* part = g.dq_part + (s * rows + id) * REC;
+    add(sum, load4(part + ch));
+    if (BF16) add(pk, load4(part + D + ch)), add(ds, load4(part + 2 * D));
+  }
+  if (BF16) {
+    sum.x = fmaf(-ds.y, pk.x, sum.x), sum.y = fmaf(-ds.y, pk.y, sum.y), sum.z = fmaf(-ds.y, pk.z, sum.z), sum.w = fmaf(-ds.y, pk.w, sum.w);
+    if (ch == 0) g.delta[g.plane + id] += ds.x;
   }
   const int row = (int)(id % a.w.Lq), bh = (int)(id / a.w.Lq);
-  put4<float>(row_of<float>(g.dq, g.sdq, bh / a.w.Hq, bh % a.w.Hq, row) + ch, make_float4(sum.x * a.scale, sum.y * a.scale, sum.z * a.scale, sum.w * a.scale));
+  put4<T>(row_of<T>(g.dq, g.sdq, bh / a.w.Hq, bh % a.w.Hq, row) + ch, make_float4(sum.x * a.scale, sum.y * a.scale, sum.z * a.scale, sum.w * a.scale));
 }
 
 template <typename F>
@@ -469,7 +477,7 @@ hipError_t launch_window_grad_f32(const WindowGradArgs& args, int d, hipStream_t
   };
   if (d == 128) go(std::integral_constant<int, 128>{});
   else go(std::integral_constant<int, 64>{});
-  return hipGetLastError();
+  return g.q_splits > 1 ? launch_window_grad_q_join(g, false, d, st) : hipGetLastError();
 }
 
 hipError_t launch_window_grad_join(const WindowGradArgs& g, bool bf16, int d, hipStream_t st) {
@@ -478,12 +486,9 @@ hipError_t launch_window_grad_join(const WindowGradArgs& g, bool bf16, int d, hi
   return by_type(bf16, d, [&](auto t, auto dc) { window_grad_join<decltype(t), decltype(dc)::value><<<grid, 256, 0, st>>>(g); });
 }
 
-hipError_t launch_window_grad_q_join(const WindowGradArgs& g, int d, hipStream_t st) {
+hipError_t launch_window_grad_q_join(const WindowGradArgs& g, bool bf16, int d, hipStream_t st) {
   const long long rows = (long long)g.f.w.B * g.f.w.Hq * g.f.w.Lq, per = 1024 / d;
-  const unsigned grid = (unsigned)((rows + per - 1) / per);
-  if (d == 128) window_grad_q_join<128><<<grid, 256, 0, st>>>(g);
-  else window_grad_q_join<64><<<grid, 256, 0, st>>>(g);
-  return hipGetLastError();
+  return by_type(bf16, d, [&](auto t, auto dc) { window_grad_q_join<decltype(t), decltype(dc)::value><<<(unsigned)((rows + per - 1) / per), 256, 0, st>>>(g); });
 }
 
 }  // namespace usv

@@ -206,7 +206,10 @@ __global__ __launch_bounds__(256, WPS) void window_grad_q_bf16(WindowGradArgs g)
     if (e + kRows <= keys.count && (e >= keys.head || e + kRows <= keys.head)) tile.load(to, ka, va, window_key(keys, e));
     else tile.load_rows(to, ka, va, [&](int r) { return (long long)window_key(keys, min(e + r, keys.count - 1)); });
   };
-  if (tiles > 0) request(0);
+  int t0 = 0, t1 = tiles;
+  if (g.q_splits > 1) t0 = (int)((long long)tiles * blockIdx.y / g.q_splits), t1 = (int)((long long)tiles * (blockIdx.y + 1) / g.q_splits);
+  t0 = __builtin_amdgcn_readfirstlane(t0), t1 = __builtin_amdgcn_readfirstlane(t1);
+  if (t0 < t1) request(t0);
 
   bf16x8 qf[2][D / 32], dof[2][D / 32];
   float nlse[2], delta[2];
@@ -232,7 +235,7 @@ __global__ __launch_bounds__(256, WPS) void window_grad_q_bf16(WindowGradArgs g)
       delta[nt] = sum_over_groups(sum);
       nlse[nt] = -a.lse[id] * kLog2e;
       range[nt] = window_range(a.w, seq.n, seq.first + some);
-      if (G == 0 && row == some) g.delta[id] = nlse[nt], g.delta[id + 2 * g.plane] = __int_as_float(range[nt].lo), g.delta[id + 3 * g.plane] = __int_as_float(range[nt].hi);
+      if (G == 0 && row == some && blockIdx.y == 0) g.delta[id] = nlse[nt], g.delta[id + 2 * g.plane] = __int_as_float(range[nt].lo), g.delta[id + 3 * g.plane] = __int_as_float(range[nt].hi);
     }
   }
   f32x16 dq[2][D / 64], pk[2][D / 64];
@@ -252,7 +255,7 @@ __global__ __launch_bounds__(256, WPS) void window_grad_q_bf16(WindowGradArgs g)
     constexpr bool OPEN = decltype(open_c)::value;
     wait_vm<0>();
     __syncthreads();  // the tile is there; everybody is done with the other stage
-    if (t + 1 < tiles) request(t + 1);
+    if (t + 1 < t1) request(t + 1);
     const unsigned char* kt = smem + (t & 1) * T::STAGE;
     const unsigned char* vt = kt + T::TENSOR;
 #pragma unroll
@@ -314,9 +317,9 @@ __global__ __launch_bounds__(256, WPS) void window_grad_q_bf16(WindowGradArgs g)
       pin(pk);
     }
   };
-  for (int t = 0; t < tiles;) {
-    for (; t < tiles && window_tile_open(keys, t * kRows, kRows); ++t) step(std::true_type{}, t);
-    for (; t < tiles && !window_tile_open(keys, t * kRows, kRows); ++t) step(std::false_type{}, t);
+  for (int t = t0; t < t1;) {
+    for (; t < t1 && window_tile_open(keys, t * kRows, kRows); ++t) step(std::true_type{}, t);
+    for (; t < t1 && !window_tile_open(keys, t * kRows, kRows); ++t) step(std::false_type{}, t);
   }
 #pragma unroll
   for (int nt = 0; nt < 2; ++nt) {
@@ -324,7 +327,22 @@ __global__ __launch_bounds__(256, WPS) void window_grad_q_bf16(WindowGradArgs g)
     if (row >= a.w.Lq) continue;
     const bool live = row >= keys.i0 && row < keys.i1;
     const float d_more = sum_over_groups(sum_ds[nt]), excess = sum_over_groups(sum_rounded[nt]);
-    if (G == 0 && live) g.delta[((long long)slot.b * a.w.Hq + slot.h) * a.w.Lq + row + g.plane] = delta[nt] + d_more;
+    const long long id = ((long long)slot.b * a.w.Hq + slot.h) * a.w.Lq + row;
+    const bool whole = g.q_splits == 1;
+    if (G == 0 && live && blockIdx.y == 0) g.delta[id + g.plane] = whole ? delta[nt] + d_more : delta[nt];
+    if (!whole) {  // (a piece: window_grad_q_join goes on)
+      constexpr int REC = window_dq_record(D);
+      float* part = g.dq_part + (blockIdx.y * ((long long)a.w.B * a.w.Hq * a.w.Lq) + id) * REC;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) {
+        const f32x4 x = quarter(dq[nt][dt >> 2], dt & 3), y = quarter(pk[nt][dt >> 2], dt & 3);
+        const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+        store4<true>(part + 16 * dt + 4 * G, live ? make_float4(x[0], x[1], x[2], x[3]) : zero, 0);
+        store4<true>(part + D + 16 * dt + 4 * G, live ? make_float4(y[0], y[1], y[2], y[3]) : zero, 0);
+      }
+      if (G == 0) store4<true>(part + 2 * D, live ? make_float4(d_more, excess, 0.f, 0.f) : make_float4(0.f, 0.f, 0.f, 0.f), 0);
+      continue;
+    }
     uint16_t* dst = row_of(g.dq, g.sdq, slot.b, slot.h, row) + 4 * G;
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) {
@@ -510,7 +528,11 @@ hipError_t run(const WindowGradArgs& args, hipStream_t st) {
   window_slots(&g.f, kBlock128);
   g.plane = (long long)g.f.w.B * g.f.w.Hq * g.f.w.Lq;
   const unsigned q_grid = (unsigned)((g.f.w.Lq + kBlock128 - 1) / kBlock128 * g.f.w.B * g.f.w.Hq);
-  if (q_grid) window_grad_q_bf16<D, WPS><<<q_grid, 256, 0, st>>>(g);
+  if (q_grid) window_grad_q_bf16<D, WPS><<<dim3(q_grid, g.q_splits), 256, 0, st>>>(g);
+  if (g.q_splits > 1) {
+    const hipError_t e = launch_window_grad_q_join(g, true, D, st);  // (the other kernel wants D)
+    if (e != hipSuccess) return e;
+  }
   if (g.blocks) window_grad_kv_bf16<D, WPS><<<window_pieces(g), 256, 0, st>>>(g);
   return hipGetLastError();
 }
