@@ -180,7 +180,9 @@ long long window_most_keys(const usv::WindowShape& s, int rows) {
 }
 
 // Pieces that the key lists of blocks of `rows` query rows are shared out in: enough to fill the chip, which runs `slots` workgroups
-// together, `least` keys each at least (a piece is a workgroup of its own, and its rows go through memory in fp32).
+// together, `least` keys each at least (a piece is a workgroup of its own, and its rows go through memory in fp32).  With the least taken / twice
+// it / half: bf16, 4 heads of 1100 rows that see all, forward 25 / 25 / 28 us (512), gradients 62 / 70 / 67 (256); fp32, 2 heads of 500
+// rows, forward 19 / 25 / 19, gradients 47 / 58 / 45 (64: a tile or two).
 int window_pieces_of(const usv::WindowShape& s, int rows, long long slots, int least) {
   const long long wgs = (long long)((s.Lq + rows - 1) / rows) * s.B * s.Hq;
   if (wgs == 0 || 2 * wgs > slots) return 1;
@@ -189,10 +191,10 @@ int window_pieces_of(const usv::WindowShape& s, int rows, long long slots, int l
   return n < 2 ? 1 : n > 256 ? 256 : (int)n;
 }
 int window_splits(const usv::WindowShape& s, int d, bool bf16) {
-  return bf16 ? window_pieces_of(s, usv::kWindowRows, d == 128 ? 1024 : 1536, 512) : window_pieces_of(s, usv::kWindowRows, 768, 256);
+  return bf16 ? window_pieces_of(s, usv::kWindowRows, d == 128 ? 1024 : 1536, 512) : window_pieces_of(s, usv::kWindowRows, 768, 64);
 }
 int window_grad_splits(const usv::WindowShape& s, int d, bool bf16) {
-  return bf16 ? window_pieces_of(s, 128, d == 128 ? 512 : 768, 512) : window_pieces_of(s, usv::kWindowRows, 512, 256);
+  return bf16 ? window_pieces_of(s, 128, d == 128 ? 512 : 768, 256) : window_pieces_of(s, usv::kWindowRows, 512, 64);
 }
 size_t window_part_bytes(const usv::WindowShape& s, int d, int splits) {
   return splits > 1 ? (size_t)splits * s.B * s.Hq * s.Lq * (d + 4) * sizeof(float) : 0;  // (d + 1, kept aligned)
