@@ -180,9 +180,9 @@ long long window_most_keys(const usv::WindowShape& s, int rows) {
 }
 
 // Pieces that the key lists of blocks of `rows` query rows are shared out in: enough to fill the chip, which runs `slots` workgroups
-// together, `least` keys each at least (a piece is a workgroup of its own, and its rows go through memory in fp32).  With the least taken / twice
-// it / half: bf16, 4 heads of 1100 rows that see all, forward 25 / 25 / 28 us (512), gradients 62 / 70 / 67 (256); fp32, 2 heads of 500
-// rows, forward 19 / 25 / 19, gradients 47 / 58 / 45 (64: a tile or two).
+// together, `least` keys each at least (a piece is a workgroup of its own, and its rows go through memory in fp32).
+// The least that the calls give, against others: bf16, 4 heads of 1100 rows that see all: forward 512 / 256 / 128 keys 25 / 28 / 30 us, gradients
+// 256 / 512 / 128 keys 62 / 70 / 67; fp32, 2 heads of 500 rows: forward 64 / 128 / 32 keys 19 / 25 / 19, gradients 47 / 58 / 45.
 int window_pieces_of(const usv::WindowShape& s, int rows, long long slots, int least) {
   const long long wgs = (long long)((s.Lq + rows - 1) / rows) * s.B * s.Hq;
   if (wgs == 0 || 2 * wgs > slots) return 1;
