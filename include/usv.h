@@ -549,7 +549,7 @@ typedef struct {
   int32_t q_start;          /* position of query row 0, at most 2^30 away from 0, or USV_Q_AT_END */
   const int32_t* seq_lens;  /* NULL, or device [B]: tokens of each sequence, clamped into [0, kv_len] */
   usv_strides q, k, v, out; /* element strides; token == 0 means contiguous [B, heads, len, d].  A stride times the element
-                               size is a multiple of 16 bytes; rows of out must not overlap */
+                               size is a multiple of 16 bytes, the token's at most 2^29 bytes; rows of out must not overlap */
 } usv_window;
 
 /* Bytes of device scratch usv_window_attn uses for `w`: 0 where the rows fill the chip; otherwise the keys are shared

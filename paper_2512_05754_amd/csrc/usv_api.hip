@@ -132,6 +132,8 @@ usv_status check_window_strides(const char* name, const usv_strides& st, int hea
   for (int i = 0; i < 3; ++i) {
     if (e[i] < 0 || e[i] > (1LL << 40)) return fail(USV_ERR_INVALID_ARG, "%s: strides must be in [0, 2^40] elements", name);
     if ((e[i] * esz) % 16 != 0) return fail(USV_ERR_INVALID_ARG, "%s: strides must be multiples of 16 bytes", name);
+    if (i == 2 && e[i] * esz > (1LL << 29))  // (the kernels reach 8 rows of a tile by a 32-bit offset)
+      return fail(USV_ERR_INVALID_ARG, "%s: the token stride must be at most 2^29 bytes", name);
     if (written && len > 0 && e[i] < d && (i < 2 || len > 1)) return fail(USV_ERR_INVALID_ARG, "%s: rows overlap (stride %lld, head_dim %d)", name, e[i], d);
   }
   *out = {e[0] * esz, e[1] * esz, e[2] * esz};

@@ -78,7 +78,7 @@ def test_no_window():
     assert binding.lib().usv_window_backward_workspace_bytes(None) == 0
 
 
-BAD_STRIDES = [UsvStrides(-8, 12800, 128), UsvStrides(102400, 12800, 132), UsvStrides(102400, (1 << 40) + 8, 128)]
+BAD_STRIDES = [UsvStrides(-8, 12800, 128), UsvStrides(102400, 12800, 132), UsvStrides(102400, (1 << 40) + 8, 128), UsvStrides(102400, 12800, (1 << 28) + 8)]
 OVERLAPS = [UsvStrides(0, 12800, 128), UsvStrides(102400, 0, 128), UsvStrides(102400, 12800, 64), UsvStrides(64, 12800, 128)]
 
 
