@@ -141,6 +141,7 @@ usv_status check_window_strides(const char* name, const usv_strides& st, int hea
 }
 
 constexpr int kMostTokens = 1 << 30;
+constexpr long long kMostWorkgroups = 0x7fffffffLL / 256;
 
 // Checks everything in `w` but the strides and fills WindowShape.
 usv_status check_window(const usv_window* w, usv::WindowShape* s) {
@@ -159,8 +160,7 @@ usv_status check_window(const usv_window* w, usv::WindowShape* s) {
     return fail(USV_ERR_INVALID_ARG, "q_start (%d) must be in [-2^30, 2^30] or USV_Q_AT_END", w->q_start);
   const long long heads = (long long)w->batch * w->q_heads;
   if (heads > 65535) return fail(USV_ERR_UNSUPPORTED, "batch * q_heads must be <= 65535");
-  if (heads * ((w->q_len > w->kv_len ? w->q_len : w->kv_len) / usv::kWindowRows + 1) > 0x7fffffffLL / 256)
-    return fail(USV_ERR_UNSUPPORTED, "batch * q_heads * length too large");
+  if (heads * (w->q_len / usv::kWindowRows + 1) > kMostWorkgroups) return fail(USV_ERR_UNSUPPORTED, "batch * q_heads * q_len too large");
   s->B = w->batch, s->Hq = w->q_heads, s->Hkv = w->kv_heads, s->group = w->q_heads / w->kv_heads;
   s->Lq = w->q_len, s->Lk = w->kv_len;
   s->left = w->left < 0 ? -1 : w->left, s->right = w->right < 0 ? -1 : w->right, s->chunk = w->chunk;
@@ -171,6 +171,15 @@ usv_status check_window(const usv_window* w, usv::WindowShape* s) {
   s->lens = w->seq_lens;
   usv::window_divs(s);
   if (reinterpret_cast<uintptr_t>(w->seq_lens) & 3u) return fail(USV_ERR_INVALID_ARG, "seq_lens is not 4-byte aligned");
+  return USV_OK;
+}
+
+// ... of the gradients, which have a workgroup per block of keys as well.
+usv_status check_window_backward(const usv_window* w, usv::WindowShape* s) {
+  const usv_status st = check_window(w, s);
+  if (st != USV_OK) return st;
+  if ((long long)w->batch * w->kv_heads * (w->kv_len / usv::kWindowRows + 1) > kMostWorkgroups)
+    return fail(USV_ERR_UNSUPPORTED, "batch * kv_heads * kv_len too large");
   return USV_OK;
 }
 
@@ -863,7 +872,7 @@ usv_status usv_window_attn(const void* q, const void* k, const void* v, const us
 
 size_t usv_window_backward_workspace_bytes(const usv_window* w) {
   usv::WindowGradArgs g = {};
-  if (check_window(w, &g.f.w) != USV_OK) return 0;
+  if (check_window_backward(w, &g.f.w) != USV_OK) return 0;
   window_grad_plan_for(&g, w);
   const bool bf16 = w->dtype == USV_BF16;
   const size_t n = window_delta_bytes(g.f.w, bf16) + window_partial_bytes(g, w->head_dim) +
@@ -876,7 +885,7 @@ usv_status usv_window_attn_backward(const void* q, const void* k, const void* v,
                                     void* dq, void* dk, void* dv, void* ws, size_t ws_bytes, void* stream) {
   usv::WindowGradArgs g = {};
   usv::WindowArgs& a = g.f;
-  USV_TRY(check_window(w, &a.w));
+  USV_TRY(check_window_backward(w, &a.w));
   if (!grads) return fail(USV_ERR_INVALID_ARG, "grads is NULL");
   const int d = w->head_dim;
   const bool bf16 = w->dtype == USV_BF16;

@@ -246,6 +246,27 @@ def test_a_cache_beyond_32_bit_offsets(usv):
     close(usv.cache_attn(q.to(DEV), cache, t.to(DEV), ints([n]), bits=bits), ref, mag, "bf16", "out")
 
 
+def test_many_sequences_with_long_tables(usv):
+    """Tables for a million positions each, of which a few are used: as with tables that just fit."""
+    B, Hq, Hkv, d, page, n = 96, 16, 2, 64, 64, 150
+    per = -(-n // page)
+    cache = usv.cache_empty(B * per, Hkv, page, d, 4)
+    short = table(B, per, B * per, seed=30).to(DEV)
+    long = torch.zeros((B, (1 << 20) // page), dtype=torch.int32, device=DEV)
+    long[:, :per] = short
+    k, v = (normal((B, Hkv, n, d), 31 + i, torch.bfloat16) for i in range(2))
+    q = normal((B, Hq, 1, d), 33, torch.bfloat16)
+    usv.cache_write(cache, k.to(DEV), v.to(DEV), long, ints([0] * B))
+    lens = ints([n - b for b in range(B)])
+    kq, vq = (wo.cache_values(f64(x), 4) for x in (k, v))
+    M = wo.masks(B, 1, n, -1, 0, 0, 1, lens=[n - b for b in range(B)])
+    ref, lse_ref, mag = wo.window_attn(f64(q), kq, vq, M)
+    for t in (short, long):
+        out, lse = usv.cache_attn(q.to(DEV), cache, t, lens, return_lse=True)
+        close(out, ref, mag, "bf16", "out")
+        close_lse(lse, lse_ref)
+
+
 @pytest.mark.parametrize("bits", [4, 8])
 def test_generation_frame_after_frame(usv, bits):
     """The operators as a streaming step uses them, captured once and replayed: write the new frame, attend to window and first frame over

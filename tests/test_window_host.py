@@ -58,7 +58,7 @@ BAD_WINDOWS = [
     (UNSUPPORTED, dict(head_dim=96)), (UNSUPPORTED, dict(head_dim=0)), (UNSUPPORTED, dict(dtype=F16)), (UNSUPPORTED, dict(dtype=-1)),
     (INVALID, dict(chunk=0)), (INVALID, dict(chunk=-5)), (INVALID, dict(chunk=MOST + 1)), (INVALID, dict(left=MOST + 1)), (INVALID, dict(right=MOST + 1)),
     (INVALID, dict(sinks=-1)), (INVALID, dict(sinks=MOST + 1)), (INVALID, dict(q_start=MOST + 1)), (INVALID, dict(q_start=-MOST - 1)), (INVALID, dict(seq_lens=FAKE + 2)),
-    (UNSUPPORTED, dict(batch=8192)), (UNSUPPORTED, dict(batch=4096, q_len=1 << 24)), (UNSUPPORTED, dict(batch=4096, kv_len=1 << 24)),
+    (UNSUPPORTED, dict(batch=8192)), (UNSUPPORTED, dict(batch=4096, q_len=1 << 24)),
 ]
 
 
@@ -70,6 +70,18 @@ def test_bad_windows(status, over):
     assert binding.lib().usv_window_workspace_bytes(ctypes.byref(w)) == 0
     assert binding.lib().usv_window_backward_workspace_bytes(ctypes.byref(w)) == 0
     assert attend(cache(), w) != 0
+
+
+def test_long_tables_are_no_reason_to_refuse():
+    """Only the gradients have workgroups per key: many sequences with tables for a million positions are an ordinary decoding batch."""
+    L = binding.lib()
+    c = cache(batch=256, kv_heads=8, table_pages=16384)
+    w = window(batch=256, q_heads=32, kv_heads=8, q_len=1, kv_len=1 << 20, left=-1, seq_lens=FAKE)
+    assert L.usv_cache_attn_workspace_bytes(ctypes.byref(c), ctypes.byref(w)) >= 0
+    assert attend(c, w, out=None) == INVALID and "out" in said()  # (as far as the pointers)
+    assert attn(w, out=None) == INVALID and "out" in said()
+    assert backward(window(batch=4096, kv_len=1 << 24)) == UNSUPPORTED and "kv_len" in said()
+    assert L.usv_window_backward_workspace_bytes(ctypes.byref(window(batch=4096, kv_len=1 << 24))) == 0
 
 
 def test_no_window():
