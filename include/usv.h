@@ -534,6 +534,7 @@ usv_status usv_block_sparse_attn_fused(const void* q, const void* k, const void*
  * queries are the newest tokens).  n = seq_lens[b], or kv_len without seq_lens.  Query rows at positions outside [0, n)
  * hold no token: out is 0 there and lse -inf; every other row sees its own position at least.  Key rows that no query of
  * a call sees and query rows without a token may hold anything, infinities and NaN among it; the others must be finite.
+ * What a call writes (workspaces too) overlaps none of its inputs.
  * Query heads h share the key head h / (q_heads / kv_heads).
  */
 #define USV_Q_AT_END INT32_MIN

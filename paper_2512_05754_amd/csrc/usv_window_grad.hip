@@ -77,8 +77,8 @@ struct Tile {
   __device__ __forceinline__ void load(unsigned lds, unsigned long long a, unsigned long long b, long long row) const {
     const int lane = lane_again();
     const unsigned chunk = ((lane & 7) ^ ((lane >> 4) << 1)) << 4;
-    const unsigned a_even = (lane >> 3) * (unsigned)a_pitch + chunk, a_odd = (lane >> 3) * (unsigned)a_pitch + (chunk ^ 16);
-    const unsigned b_even = (lane >> 3) * (unsigned)b_pitch + chunk, b_odd = (lane >> 3) * (unsigned)b_pitch + (chunk ^ 16);
+    const unsigned a_even = (lane >> 3) * (unsigned)a_pitch + chunk, a_odd = (lane >> 3) * (unsigned)a_pitch + (chunk ^ 80);
+    const unsigned b_even = (lane >> 3) * (unsigned)b_pitch + chunk, b_odd = (lane >> 3) * (unsigned)b_pitch + (chunk ^ 80);
     const unsigned long long a0 = a + (row + 16 * wave) * a_pitch, b0 = b + (row + 16 * wave) * b_pitch;
     const unsigned to = lds + 16 * wave * 128;
 #pragma unroll
@@ -100,7 +100,7 @@ struct Tile {
 #pragma unroll 1
     for (int r = 0; r < 2; ++r) {
       const long long row = row_at(16 * wave + 8 * r + (lane >> 3));
-      const unsigned chunk = ((lane & 7) ^ (((lane >> 4) << 1) | r)) << 4;
+      const unsigned chunk = ((lane & 7) ^ ((lane >> 4) << 1) ^ (5 * r)) << 4;
 #pragma unroll
       for (int line = 0; line < LINES; ++line) {
         dma_lane(to + line * kLine + 1024 * r, a + row * a_pitch + line * 128 + chunk);
@@ -115,9 +115,9 @@ struct Lanes {
   unsigned rows, columns;
   __device__ __forceinline__ void init() {
     const int lane = threadIdx.x & 63, c = lane & 15, G = lane >> 4;
-    rows = c * 128 + ((G ^ ((((c >> 1) & 3) << 1) | (c >> 3))) << 4);
+    rows = c * 128 + ((G ^ (((c >> 1) & 3) << 1) ^ (5 * (c >> 3))) << 4);
     const int row = 4 * G + (c >> 2), p = row >> 1;
-    columns = row * 128 + ((((c & 3) >> 1) ^ (((p & 3) << 1) | (p >> 2))) << 4) + (c & 1) * 8;
+    columns = row * 128 + ((((c & 3) >> 1) ^ ((p & 3) << 1) ^ (5 * (p >> 2))) << 4) + (c & 1) * 8;
   }
   __device__ __forceinline__ bf16x8 row_frag(const unsigned char* tensor, int sub, int m, int t) const {
     return *reinterpret_cast<const bf16x8*>(tensor + (rows ^ ((t & 1) << 6)) + (t >> 1) * kLine + (32 * sub + 16 * m) * 128);
