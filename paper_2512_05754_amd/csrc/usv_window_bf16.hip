@@ -19,6 +19,9 @@
 // other steps compute a full address per lane.
 //
 // The weights are rounded to bf16 for the second product; their sum is taken unrounded, in fp32.
+//
+// What bounds it: the matrix pipes at the chip's power limit.  12 heads, d = 128: 480p frames (32760 tokens, left 6, one sink frame) 1.94 ms, 720p frames (75600,
+// left and right 3) 11.1 ms: 1.08 and 1.09 PFLOP/s, where a product of 8192^3 Gaussian values runs at 1.35.  A list of few tiles: 1.5 us a masked step.
 #include "usv_attn_bf16.h"
 #include "usv_window.h"
 

@@ -15,7 +15,8 @@
 // P and dS are formed twice and nothing is added with atomics, so a call repeats its bits.  Rows that hold no token are never
 // contracted over: row and key indices are clamped to ones that some partner sees, and the mask takes the doubles out.
 //
-// What bounds it: the fp32 matrix cores (154 TFLOP/s in an 8192-cubed product).
+// What bounds it: the fp32 matrix cores (154 TFLOP/s in an 8192-cubed product).  2 heads of 4095 tokens, left 1023, d = 128: forward 51 us, query
+// rows 70, keys 96 (74, 81 and 79 TFLOP/s of the products formed), the joins 7, 5 and 10.
 #include "usv_attn_bf16.h"
 #include "usv_window.h"
 
@@ -25,10 +26,6 @@ namespace {
 constexpr int kTile = 32;  // keys (key gradient: query rows) of a step
 
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 load4(const uint16_t* p) {
-  const uint2 x = *reinterpret_cast<const uint2*>(p);
-  return bf16_pair(x.x, x.y);
-}
 template <typename T>
 __device__ __forceinline__ void put4(void* p, const float4& x) {
   store4<std::is_same<T, float>::value>(p, x, 0);
@@ -45,11 +42,11 @@ __device__ __forceinline__ float at(const float4& x, int e) { return e == 0 ? x.
 __device__ __forceinline__ f32x4 mfma(float a, float b, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
 // A tile of kTile rows of two tensors, on its way to LDS: thread t holds channels 4 (t % 8) + 32 x of row t / 8.
-template <typename T, int D>
+template <int D>
 struct Pair {
   static constexpr int X = D / 32, PITCH = D + 4;
   float4 a[X], b[X];
-  __device__ __forceinline__ void load(const T* ra, const T* rb) {
+  __device__ __forceinline__ void load(const float* ra, const float* rb) {
     const int c = 4 * (threadIdx.x & 7);
 #pragma unroll
     for (int x = 0; x < X; ++x) a[x] = load4(ra + c + 32 * x), b[x] = load4(rb + c + 32 * x);
@@ -89,7 +86,7 @@ __device__ __forceinline__ void columns_times(const float* tile, const f32x4 (&p
       for (int dt = 0; dt < D / 16; ++dt) o[dt] = mfma(tile[(16 * m + 4 * G + r) * (D + 4) + 16 * dt + c], p[m][r], o[dt]);
 }
 
-template <typename T, int D>
+template <int D>
 __global__ __launch_bounds__(256) void window_fwd(WindowArgs a) {
   __shared__ __attribute__((aligned(16))) float sk[kTile * (D + 4)], sv[kTile * (D + 4)];
   const int blocks = (a.w.Lq + kWindowRows - 1) / kWindowRows;
@@ -113,13 +110,13 @@ __global__ __launch_bounds__(256) void window_fwd(WindowArgs a) {
     const int qrow = min(max(row, keys.i0), keys.i1 - 1);
     const WindowRange range = window_range(a.w, seq.n, seq.first + qrow);
     float4 qf[D / 16];
-    const T* qp = row_of<T>(a.q, a.sq, at_.b, at_.h, qrow) + 4 * G;
+    const float* qp = row_of<float>(a.q, a.sq, at_.b, at_.h, qrow) + 4 * G;
 #pragma unroll
     for (int u = 0; u < D / 16; ++u) qf[u] = load4(qp + 16 * u);
-    Pair<T, D> next;
+    Pair<D> next;
     auto fetch = [&](int t) {
       const long long key = window_key(keys, min(t * kTile + (int)(threadIdx.x >> 3), keys.count - 1));
-      next.load(row_of<T>(a.k, a.sk, at_.b, hk, key), row_of<T>(a.v, a.sv, at_.b, hk, key));
+      next.load(row_of<float>(a.k, a.sk, at_.b, hk, key), row_of<float>(a.v, a.sv, at_.b, hk, key));
     };
     fetch(t0);
     for (int t = t0; t < t1; ++t) {
@@ -166,12 +163,12 @@ __global__ __launch_bounds__(256) void window_fwd(WindowArgs a) {
   const long long rows = (long long)a.w.B * a.w.Hq * a.w.Lq, id = ((long long)at_.b * a.w.Hq + at_.h) * a.w.Lq + row;
   const bool parts = a.splits > 1;
   unsigned char* dst = parts ? reinterpret_cast<unsigned char*>(a.part_o + (blockIdx.y * rows + id) * D)
-                             : reinterpret_cast<unsigned char*>(row_of<T>(a.out, a.so, at_.b, at_.h, row));
+                             : reinterpret_cast<unsigned char*>(row_of<float>(a.out, a.so, at_.b, at_.h, row));
 #pragma unroll
   for (int dt = 0; dt < D / 16; ++dt) {
     const float4 x = some ? make_float4(o[dt][0] * inv, o[dt][1] * inv, o[dt][2] * inv, o[dt][3] * inv) : make_float4(0.f, 0.f, 0.f, 0.f);
     if (parts) put4<float>(dst + (16 * dt + 4 * G) * 4, x);
-    else put4<T>(dst + (16 * dt + 4 * G) * sizeof(T), x);
+    else put4<float>(dst + (16 * dt + 4 * G) * sizeof(float), x);
   }
   if (G == 0) {
     if (parts) a.part_lse[blockIdx.y * rows + id] = lse;
@@ -228,7 +225,7 @@ __global__ __launch_bounds__(256) void window_join(WindowArgs a) {
   if (a.lse && ch == 0) a.lse[id] = m == -INFINITY ? -INFINITY : m + __log2f(l) * kLn2;
 }
 
-template <typename T, int D>
+template <int D>
 __global__ __launch_bounds__(256) void window_grad_q(WindowGradArgs g) {
   const WindowArgs& a = g.f;
   __shared__ __attribute__((aligned(16))) float sk[kTile * (D + 4)], sv[kTile * (D + 4)];
@@ -251,9 +248,9 @@ __global__ __launch_bounds__(256) void window_grad_q(WindowGradArgs g) {
     const int qrow = min(max(row, keys.i0), keys.i1 - 1);
     const WindowRange range = window_range(a.w, seq.n, seq.first + qrow);
     float4 qf[D / 16], dof[D / 16];
-    const T* qp = row_of<T>(a.q, a.sq, at_.b, at_.h, qrow) + 4 * G;
-    const T* dop = row_of<T>(g.dout, g.sdo, at_.b, at_.h, qrow) + 4 * G;
-    const T* op = row_of<T>(static_cast<const void*>(a.out), a.so, at_.b, at_.h, qrow) + 4 * G;
+    const float* qp = row_of<float>(a.q, a.sq, at_.b, at_.h, qrow) + 4 * G;
+    const float* dop = row_of<float>(g.dout, g.sdo, at_.b, at_.h, qrow) + 4 * G;
+    const float* op = row_of<float>(static_cast<const void*>(a.out), a.so, at_.b, at_.h, qrow) + 4 * G;
     float delta = 0.f;
 #pragma unroll
     for (int u = 0; u < D / 16; ++u) {
@@ -265,10 +262,10 @@ __global__ __launch_bounds__(256) void window_grad_q(WindowGradArgs g) {
     delta = sum_over_groups(delta);
     if (G == 0 && live && blockIdx.y == 0) g.delta[id] = delta;
     const float sl = a.scale * kLog2e, ref = a.lse[((long long)at_.b * a.w.Hq + at_.h) * a.w.Lq + qrow] * kLog2e;
-    Pair<T, D> next;
+    Pair<D> next;
     auto fetch = [&](int t) {
       const long long key = window_key(keys, min(t * kTile + (int)(threadIdx.x >> 3), keys.count - 1));
-      next.load(row_of<T>(a.k, a.sk, at_.b, hk, key), row_of<T>(a.v, a.sv, at_.b, hk, key));
+      next.load(row_of<float>(a.k, a.sk, at_.b, hk, key), row_of<float>(a.v, a.sv, at_.b, hk, key));
     };
     if (t0 < t1) fetch(t0);
     for (int t = t0; t < t1; ++t) {
@@ -298,15 +295,15 @@ __global__ __launch_bounds__(256) void window_grad_q(WindowGradArgs g) {
     for (int dt = 0; dt < D / 16; ++dt) put4<float>(part + 16 * dt, live ? make_float4(dq[dt][0], dq[dt][1], dq[dt][2], dq[dt][3]) : make_float4(0.f, 0.f, 0.f, 0.f));
     return;
   }
-  T* dst = row_of<T>(g.dq, g.sdq, at_.b, at_.h, row);
+  float* dst = row_of<float>(g.dq, g.sdq, at_.b, at_.h, row);
 #pragma unroll
   for (int dt = 0; dt < D / 16; ++dt) {
     const float4 x = live ? make_float4(dq[dt][0] * a.scale, dq[dt][1] * a.scale, dq[dt][2] * a.scale, dq[dt][3] * a.scale) : make_float4(0.f, 0.f, 0.f, 0.f);
-    put4<T>(dst + 16 * dt + 4 * G, x);
+    put4<float>(dst + 16 * dt + 4 * G, x);
   }
 }
 
-template <typename T, int D>
+template <int D>
 __global__ __launch_bounds__(256) void window_grad_kv(WindowGradArgs g) {
   const WindowArgs& a = g.f;
   constexpr int KB = 64;
@@ -328,17 +325,17 @@ __global__ __launch_bounds__(256) void window_grad_kv(WindowGradArgs g) {
   if (n0 < n1) {
     const int krow = min(key, seq.n - 1);
     float4 kf[D / 16], vf[D / 16];
-    const T* kp = row_of<T>(a.k, a.sk, pc.b, pc.h, krow) + 4 * G;
-    const T* vp = row_of<T>(a.v, a.sv, pc.b, pc.h, krow) + 4 * G;
+    const float* kp = row_of<float>(a.k, a.sk, pc.b, pc.h, krow) + 4 * G;
+    const float* vp = row_of<float>(a.v, a.sv, pc.b, pc.h, krow) + 4 * G;
 #pragma unroll
     for (int u = 0; u < D / 16; ++u) kf[u] = load4(kp + 16 * u), vf[u] = load4(vp + 16 * u);
     const float sl = a.scale * kLog2e;
-    Pair<T, D> next;
+    Pair<D> next;
     float4 next_row = make_float4(0.f, 0.f, 0.f, 0.f);
     auto fetch = [&](int n) {
       const int h = pc.h * a.w.group + n / tiles, i = rows.i0 + (n % tiles) * kTile + (int)(threadIdx.x >> 3);
       const int row = min(i, rows.i1 - 1);
-      next.load(row_of<T>(a.q, a.sq, pc.b, h, row), row_of<T>(g.dout, g.sdo, pc.b, h, row));
+      next.load(row_of<float>(a.q, a.sq, pc.b, h, row), row_of<float>(g.dout, g.sdo, pc.b, h, row));
       if ((threadIdx.x & 7) == 0) {
         const long long id = ((long long)pc.b * a.w.Hq + h) * a.w.Lq + row;
         const WindowRange r = i < rows.i1 ? window_range(a.w, seq.n, seq.first + i) : WindowRange{0, 0};
@@ -378,12 +375,12 @@ __global__ __launch_bounds__(256) void window_grad_kv(WindowGradArgs g) {
       put4<float>(dst + KB * D + 16 * dt, make_float4(dv[dt][0], dv[dt][1], dv[dt][2], dv[dt][3]));
     }
   } else if (key < a.w.Lk) {
-    T* pk = row_of<T>(g.dk, g.sdk, pc.b, pc.h, key) + 4 * G;
-    T* pv = row_of<T>(g.dv, g.sdv, pc.b, pc.h, key) + 4 * G;
+    float* pk = row_of<float>(g.dk, g.sdk, pc.b, pc.h, key) + 4 * G;
+    float* pv = row_of<float>(g.dv, g.sdv, pc.b, pc.h, key) + 4 * G;
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) {
-      put4<T>(pk + 16 * dt, make_float4(dk[dt][0] * a.scale, dk[dt][1] * a.scale, dk[dt][2] * a.scale, dk[dt][3] * a.scale));
-      put4<T>(pv + 16 * dt, make_float4(dv[dt][0], dv[dt][1], dv[dt][2], dv[dt][3]));
+      put4<float>(pk + 16 * dt, make_float4(dk[dt][0] * a.scale, dk[dt][1] * a.scale, dk[dt][2] * a.scale, dk[dt][3] * a.scale));
+      put4<float>(pv + 16 * dt, make_float4(dv[dt][0], dv[dt][1], dv[dt][2], dv[dt][3]));
     }
   }
 }
@@ -453,8 +450,8 @@ hipError_t launch_window_f32(const WindowArgs& args, int d, hipStream_t st) {
   WindowArgs a = args;
   window_slots(&a, kWindowRows);
   const dim3 grid((unsigned)((a.w.Lq + kWindowRows - 1) / kWindowRows * a.w.B * a.w.Hq), a.splits);
-  if (d == 128) window_fwd<float, 128><<<grid, 256, 0, st>>>(a);
-  else window_fwd<float, 64><<<grid, 256, 0, st>>>(a);
+  if (d == 128) window_fwd<128><<<grid, 256, 0, st>>>(a);
+  else window_fwd<64><<<grid, 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -472,8 +469,8 @@ hipError_t launch_window_grad_f32(const WindowGradArgs& args, int d, hipStream_t
   const unsigned q_grid = (unsigned)((g.f.w.Lq + kWindowRows - 1) / kWindowRows * g.f.w.B * g.f.w.Hq);
   auto go = [&](auto dc) {
     constexpr int D = decltype(dc)::value;
-    if (q_grid) window_grad_q<float, D><<<dim3(q_grid, g.q_splits), 256, 0, st>>>(g);
-    if (g.blocks) window_grad_kv<float, D><<<window_pieces(g), 256, 0, st>>>(g);
+    if (q_grid) window_grad_q<D><<<dim3(q_grid, g.q_splits), 256, 0, st>>>(g);
+    if (g.blocks) window_grad_kv<D><<<window_pieces(g), 256, 0, st>>>(g);
   };
   if (d == 128) go(std::integral_constant<int, 128>{});
   else go(std::integral_constant<int, 64>{});

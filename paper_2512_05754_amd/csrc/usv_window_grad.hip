@@ -25,6 +25,9 @@
 // (transposed); chunk k of row i lies at k ^ f(i / 2 % 8), f(p) = 2 (p % 4) + p / 4, which keeps both free of bank conflicts.
 //
 // P and dS are rounded to bf16 for the second product, nothing else is; sums are fp32.
+//
+// What bounds it: as the forward pass, power and the pipes.  480p frames (12 heads, 32760 tokens, left 6, one sink frame): query rows 3.6 ms, keys 3.6 ms,
+// 1.16 PFLOP/s each (matrix pipes busy 52 % at 2.07 GHz); 4 x 16 heads on 4, 2047 tokens, left 511, d = 64: 49 and 56 us.
 #include "usv_attn_bf16.h"
 #include "usv_window.h"
 
