@@ -47,8 +47,8 @@ __device__ __forceinline__ void dma_rows(unsigned lds, const unsigned long long 
       "global_load_lds_dwordx4 %1, %5 offset:%9\n\t"
       "global_load_lds_dwordx4 %2, %6 offset:%10"
       :
-      : "s"(lds - 128 * LINE), "v"(even), "v"(odd), "s"(base[0]), "s"(base[1]), "s"(base[2]), "s"(base[3]), "n"(128 * LINE), "n"(1024 + 128 * LINE), "n"(2048 + 128 * LINE),
-        "n"(3072 + 128 * LINE)
+      : "s"(lds - 128 * LINE), "v"(even), "v"(odd), "s"(base[0]), "s"(base[1]), "s"(base[2]), "s"(base[3]), "n"(128 * LINE), "n"(1024 + 128 * LINE), "n"(2 * 1024 + 128 * LINE),
+        "n"(3 * 1024 + 128 * LINE)
       : "memory");
 }
 __device__ __forceinline__ void dma_lane(unsigned lds, unsigned long long addr) {  // 64 lanes, an address each
