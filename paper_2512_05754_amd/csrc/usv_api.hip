@@ -183,13 +183,6 @@ usv_status check_window_backward(const usv_window* w, usv::WindowShape* s) {
   return USV_OK;
 }
 
-// Keys that a block of `rows` query rows sees at most.
-long long window_most_keys(const usv::WindowShape& s, int rows) {
-  if (s.left < 0 || s.right < 0) return s.Lk;
-  const long long n = s.sink + ((long long)s.left + s.right + 1) * s.chunk + rows + s.chunk;
-  return n < s.Lk ? n : s.Lk;
-}
-
 // Pieces that the key lists of blocks of `rows` query rows are shared out in: enough to fill the chip, which runs `slots` workgroups
 // together, `least` keys each at least (a piece is a workgroup of its own, and its rows go through memory in fp32).
 // The least that the calls give, against others: bf16, 4 heads of 1100 rows that see all: forward 512 / 256 / 128 keys 25 / 28 / 30 us, gradients
@@ -197,7 +190,7 @@ long long window_most_keys(const usv::WindowShape& s, int rows) {
 int window_pieces_of(const usv::WindowShape& s, int rows, long long slots, int least) {
   const long long wgs = (long long)((s.Lq + rows - 1) / rows) * s.B * s.Hq;
   if (wgs == 0 || 2 * wgs > slots) return 1;
-  const long long by_slots = slots / wgs, by_keys = window_most_keys(s, rows) / least;
+  const long long by_slots = slots / wgs, by_keys = usv::window_most_keys(s, rows) / least;
   const long long n = by_slots < by_keys ? by_slots : by_keys;
   return n < 2 ? 1 : n > 256 ? 256 : (int)n;
 }
@@ -304,7 +297,7 @@ usv_status check_cache_attn(const usv_cache* c, const usv_window* w, usv::CacheS
 int cache_attn_splits(const usv::WindowShape& s) {
   const int rows = usv::cache_attn_rows(s);
   const long long all = (long long)s.Lq * s.group, wgs = (all + rows - 1) / rows * s.B * s.Hkv;
-  const long long target = rows == 16 ? 2048 : 512, by_keys = window_most_keys(s, rows) / 512;
+  const long long target = rows == 16 ? 2048 : 512, by_keys = usv::window_most_keys(s, rows) / 512;
   if (wgs == 0 || 2 * wgs > target) return 1;
   const long long by_wgs = target / wgs, n = by_wgs < by_keys ? by_wgs : by_keys;
   return n < 2 ? 1 : n > 256 ? 256 : (int)n;
@@ -315,7 +308,7 @@ int cache_attn_splits(const usv::WindowShape& s) {
 // 15600 keys in 8 bits, 256 rows 54 / 72 us, 512 84 / 91, 1024 174 / 130, 4680 657 / 500; in 4 bits, 512 74 / 87, 1024 151 / 125; 4 x 8 key heads of 8192
 // keys, 512 rows 92 / 108, 1024 152 / 164; d = 64: 2 x 16 key heads, 512 rows 73 / 72.  Copies beyond 1 GiB are not made.
 long long cache_attn_copy(const usv::CacheShape& c, const usv::WindowShape& s) {
-  const long long rows = window_most_keys(s, s.Lq), bytes = 4 * rows * s.B * s.Hkv * c.d;
+  const long long rows = usv::window_most_keys(s, s.Lq), bytes = 4 * rows * s.B * s.Hkv * c.d;
   return (long long)s.Lq * s.group >= 1024 && bytes <= (1LL << 30) ? rows : 0;
 }
 size_t cache_attn_copy_bytes(const usv::CacheShape& c, long long rows) { return (size_t)4 * rows * c.B * c.H * c.d; }

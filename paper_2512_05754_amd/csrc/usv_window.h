@@ -212,6 +212,13 @@ __device__ __forceinline__ WindowPiece window_piece(const WindowGradArgs& g, int
   return p;
 }
 
+// Keys that a block of `rows` query rows sees at most.
+inline long long window_most_keys(const WindowShape& s, int rows) {
+  if (s.left < 0 || s.right < 0) return s.Lk;
+  const long long n = s.sink + ((long long)s.left + s.right + 1) * s.chunk + rows + s.chunk;
+  return n < s.Lk ? n : s.Lk;
+}
+
 constexpr int kWindowRows = 64;  // query rows of a workgroup
 
 hipError_t launch_window_f32(const WindowArgs& a, int d, hipStream_t st);

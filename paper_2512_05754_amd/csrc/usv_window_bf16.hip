@@ -1,7 +1,7 @@
 // Windowed attention with sinks, bf16, forward.
 //
-// One workgroup = 2 wavefronts = 64 query rows of one head.  Wave w owns all 64 rows and every other stretch of 32 entries of the block's
-// key list, with an online softmax of its own; the two results are merged once, at the end.  A wave fetches, waits for and
+// One workgroup = 2 wavefronts (4 where workgroups are few) = 64 query rows of one head.  Wave w owns all 64 rows and every other (fourth) stretch of
+// 32 entries of the block's key list, with an online softmax of its own; the results are merged once, at the end.  A wave fetches, waits for and
 // reads its own K and V only, so the main loop has no barrier, and a fragment read from LDS feeds four MFMAs.
 //
 // Matrix cores (v_mfma_f32_16x16x32_bf16; lane = (c, G), c = lane % 16, G = lane / 16):
@@ -28,7 +28,6 @@
 namespace usv {
 namespace {
 
-constexpr int NW = 2;
 constexpr int kItem = 4096;
 constexpr int kStep = 32;                // entries of a wave's step
 template <int D>
@@ -76,8 +75,9 @@ __device__ __forceinline__ ArgsAgain again() {
 
 // QL: Q fragments of the last channel step that are read back from LDS, four more reads a step.  All of Q in registers is 1 to 2 % faster where
 // every step is hot, but the other steps then spill: 480p frames, left 6, 1.94 ms against 2.05 (QL = 2: 1.99); d = 64, window 1000, 97.3 against 102.9 us.
-template <int D, int WPS, int QL, bool CIRCLE>
+template <int D, int NW, int WPS, int QL, bool CIRCLE>
 __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
+  constexpr int TILE = NW * kStep;  // entries that the waves work on together
   constexpr int KS = D / 32, DT = D / 16, OT = (DT + 3) / 4;
   constexpr int LINES = D / 64, IPS = 2 * LINES;
   constexpr int KF = 3, VF = 2;  // fragments of K, V in flight
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   const int lane = threadIdx.x & 63, c16 = lane & 15, G = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  // Entries of this workgroup: tiles of 64 that end where the list does; what is missing from a whole number of them is missing ahead of
+  // Entries of this workgroup: tiles of TILE that end where the list does; what is missing from a whole number of them is missing ahead of
   // entry 0.  This wave's half of tile t begins at entry entry_of(t).
   // CIRCLE: workgroups that run together have windows that lie one behind the other.  Each begun at its own first key, they read a key at
   // different times, and the L2 has lost it in between.  So the window's tiles are walked in a circle, from the first key that is a multiple of
@@ -109,17 +109,17 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   // and the rounds, whose starts spread by about 0.3 sqrt(round) of a sweep; a workgroup begins as much further on as its place in the round is
   // expected to be late.  (720p frames, left and right 3: 15.4 ms; circle 15.1, with turns 14.3, starts spread by 0.2 / 0.3 / 0.5
   // sqrt(round) 12.4 / 11.7 / 11.8.)
-  const int tiles = (keys.count + 63) / 64;
+  const int tiles = (keys.count + TILE - 1) / TILE;
   int t0 = 0, t1 = tiles;
   if (a.splits > 1) t0 = (int)((long long)tiles * blockIdx.y / a.splits), t1 = (int)((long long)tiles * (blockIdx.y + 1) / a.splits);
   t0 = __builtin_amdgcn_readfirstlane(t0);
   const int n_steps = __builtin_amdgcn_readfirstlane(t1) - t0;
-  const int start = keys.count - tiles * 64;  // of tile 0
-  const int head_tiles = keys.head > 0 ? (keys.head - start + 63) / 64 : 0;
+  const int start = keys.count - tiles * TILE;  // of tile 0
+  const int head_tiles = keys.head > 0 ? (keys.head - start + TILE - 1) / TILE : 0;
   int turn = 0;  // tiles between the window's first and the one that the circle begins with
   if (CIRCLE && tiles > head_tiles) {
     const int lo = keys.head + keys.skip, key = (lo + a.period - 1) / a.by_period * a.period;
-    if (key < keys.count + keys.skip) turn = max(0, (key - keys.skip - start) / 64 - head_tiles);
+    if (key < keys.count + keys.skip) turn = max(0, (key - keys.skip - start) / TILE - head_tiles);
     const int rank = blockIdx.x / kNumXcd, round = rank / kTogether<D>;
     const float at = fminf(1.f, 0.3f * __builtin_amdgcn_sqrtf((float)round)) * ((float)(rank - round * kTogether<D>) * (1.f / kTogether<D>) - 0.5f);
     const int n = tiles - head_tiles;
@@ -135,7 +135,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
     }
     return t;
   };
-  auto entry_of = [&](int t) { return start + 64 * t + wave * kStep; };
+  auto entry_of = [&](int t) { return start + TILE * t + wave * kStep; };
 
   if (threadIdx.x < kWindowRows) {
     const int row = row0 + threadIdx.x;
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
       vb[r] = uniform(vb0 + (key + 8 * r) * b->sv.token - 1024 * r);
     }
   };
-  const unsigned long long kmove = uniform(64ull * a.sk.token), vmove = uniform(64ull * a.sv.token);
+  const unsigned long long kmove = uniform((unsigned long long)TILE * a.sk.token), vmove = uniform((unsigned long long)TILE * a.sv.token);
   auto plain_step = [&](int e) { return e >= keys.head || (e >= 0 && e + kStep <= keys.head); };
   // item x of the step that kb, vb point at
   auto dma = [&](auto x_c) {
@@ -253,7 +253,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
     for (int t = 0; t < KS; ++t)
       if (t < KS - 1 || nt < 4 - QL) asm volatile("" : "+v"(qf[nt][t]));  // (else their loads sink into the loop, with waits for all memory)
 
-  // One step.  HOT: every row sees all its keys, and the next step lies 64 keys further on; that one is fetched item by item while this one
+  // One step.  HOT: every row sees all its keys, and the next step lies TILE keys further on; that one is fetched item by item while this one
   // is worked on.  Otherwise (a few steps of a list: its ends and the diagonal) the mask is applied, and the next step is fetched behind this one if
   // its rows need addresses of their own.
   auto step = [&](auto hot_c, int n) {
@@ -410,9 +410,9 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
     const int t = tile_of(n), e0 = entry_of(t), key = window_key(keys, e0);
     if (e0 < 0 || (key < keys.all_lo && key >= keys.all_sink)) return 0;
     const int open = e0 < keys.head || key < keys.all_lo ? keys.all_sink : keys.all_hi;  // (keys below are seen by every row)
-    int k = min(n_steps - 1 - n, (open - key + kStep) / 64);  // the step's keys lie below
+    int k = min(n_steps - 1 - n, (open - key + TILE - kStep) / TILE);  // the step's keys lie below
     k = min(k, (t < head_tiles ? head_tiles : tiles) - 1 - t);  // the next tile is the one behind it
-    if (e0 < keys.head) k = min(k, (keys.head - e0 - kStep) / 64);                         // the next step's too
+    if (e0 < keys.head) k = min(k, (keys.head - e0 - kStep) / TILE);                         // the next step's too
     return max(k, 0);
   };
   unsigned pace = CIRCLE ? __builtin_amdgcn_s_getreg(4 | (3 << 11)) : 0;  // HW_ID, bits 0..3: the wave's slot of its SIMD
@@ -438,17 +438,18 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   }
   const ArgsAgain z = again();
 
-  // ---- merge the two waves, stage the rows in LDS, store ----
-  // Wave w finishes query tiles 2 w and 2 w + 1: it gives the other two away through its own area (dead by now), adds what the other wave
-  // gave, and stages its rows where it has just read.
+  // ---- merge the waves, stage the rows in LDS, store ----
+  // Of waves 2 x and 2 x + 1 the first takes query tiles 0 and 1, the second 2 and 3: each gives the other two away through its own area
+  // (dead by now) and adds what the other gave.  Of four waves, x and x + 2 then share the two tiles that both have in the same way.  The rows
+  // are staged where the wave has just read.
   float l_row[4];
 #pragma unroll
   for (int nt = 0; nt < 4; ++nt) l_row[nt] = sum_over_groups(l[nt]);
-  auto give = [&](auto first_c) {
-    constexpr int F = decltype(first_c)::value;
+  auto give = [&](auto first_c, auto count_c) {
+    constexpr int F = decltype(first_c)::value, N = decltype(count_c)::value;
     float* dst = reinterpret_cast<float*>(smem + wave * kWaveBytes) + lane;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
+    for (int e = 0; e < N; ++e) {
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -459,16 +460,26 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
   };
   const long long rows = (long long)z->w.B * z->w.Hq * z->w.Lq, id0 = ((long long)slot.b * z->w.Hq + slot.h) * z->w.Lq;
   const bool parts = z->splits > 1;
-  auto take = [&](auto first_c) {
-    constexpr int F = decltype(first_c)::value;
-    float* area = reinterpret_cast<float*>(smem + (wave ^ 1) * kWaveBytes);
+  auto take = [&](auto first_c, auto count_c, auto last_c, int from) {
+    constexpr int F = decltype(first_c)::value, N = decltype(count_c)::value;
+    constexpr bool LAST = decltype(last_c)::value;
+    float* area = reinterpret_cast<float*>(smem + from * kWaveBytes);
     const float* src = area + lane;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
+    for (int e = 0; e < N; ++e) {
       const float n1 = src[(DT * 8 + e) * 64], l1 = src[(DT * 8 + 2 + e) * 64];
       const float ref = fminf(nm[F + e], n1);
       const float a0 = fast_exp2(ref - nm[F + e]), a1 = fast_exp2(ref - n1);  // (a side without keys: l = 0, O = 0)
       const float lt = l_row[F + e] * a0 + l1 * a1;
+      if constexpr (!LAST) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            o[F + e][dt >> 2][4 * (dt & 3) + r] = o[F + e][dt >> 2][4 * (dt & 3) + r] * a0 + src[((e * DT + dt) * 4 + r) * 64] * a1;
+        nm[F + e] = ref, l_row[F + e] = lt;
+        continue;
+      }
       const int row = row0 + 16 * (F + e) + c16;
       const bool live = row >= keys.i0 && row < keys.i1 && lt > 0.f;
       const float inv = live ? 1.f / lt : 0.f;
@@ -486,9 +497,10 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
         else if (z->lse) z->lse[id0 + row] = val;
       }
     }
+    if constexpr (!LAST) return;
     wait_lds<0>();  // every exchange value of this wave is in registers before its area is overwritten
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
+    for (int e = 0; e < N; ++e) {
       float* stage = area + (16 * e + c16) * OSTRIDE;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
@@ -499,16 +511,31 @@ __global__ __launch_bounds__(64 * NW, WPS) void window_fwd_bf16(WindowArgs a) {
     }
   };
   __syncthreads();  // (the other wave's last reads of its area are its own; the areas are given away only behind both loops)
-  if (wave == 0) give(I2{});
-  else give(I0{});
+  if ((wave & 1) == 0) give(I2{}, I2{});
+  else give(I0{}, I2{});
   __syncthreads();
-  if (wave == 0) take(I0{});
-  else take(I2{});
-  const float* other = reinterpret_cast<const float*>(smem + (wave ^ 1) * kWaveBytes);
+  using Last = std::bool_constant<NW == 2>;
+  if ((wave & 1) == 0) take(I0{}, I2{}, Last{}, wave ^ 1);
+  else take(I2{}, I2{}, Last{}, wave ^ 1);
+  if constexpr (NW == 4) {
+    __syncthreads();
+    if (wave == 0) give(I1{}, I1{});
+    else if (wave == 1) give(I3{}, I1{});
+    else if (wave == 2) give(I0{}, I1{});
+    else give(I2{}, I1{});
+    __syncthreads();
+    if (wave == 0) take(I0{}, I1{}, std::true_type{}, 2);
+    else if (wave == 1) take(I2{}, I1{}, std::true_type{}, 3);
+    else if (wave == 2) take(I1{}, I1{}, std::true_type{}, 0);
+    else take(I3{}, I1{}, std::true_type{}, 1);
+  }
+  constexpr int MINE = 64 / NW;  // rows
+  const int first = NW == 2 ? 32 * wave : 32 * (wave & 1) + 16 * (wave >> 1);
+  const float* other = reinterpret_cast<const float*>(smem + (wave ^ (NW / 2)) * kWaveBytes);
   unsigned char* const dst = static_cast<unsigned char*>(z->out) + slot.b * z->so.batch + slot.h * z->so.head;
 #pragma unroll
-  for (int it = 0; it < 32 * D / 8 / 64; ++it) {
-    const int id = it * 64 + lane, rr = id / (D / 8), ch = (id % (D / 8)) * 8, row = row0 + 32 * wave + rr;
+  for (int it = 0; it < MINE * D / 8 / 64; ++it) {
+    const int id = it * 64 + lane, rr = id / (D / 8), ch = (id % (D / 8)) * 8, row = row0 + first + rr;
     if (row >= z->w.Lq) continue;
     const float4 val[2] = {*reinterpret_cast<const float4*>(other + rr * OSTRIDE + ch), *reinterpret_cast<const float4*>(other + rr * OSTRIDE + ch + 4)};
     if (parts) store8<true>(z->part_o + (blockIdx.y * rows + id0 + row) * D + ch, val, 0);
@@ -533,12 +560,18 @@ hipError_t launch_window_bf16(const WindowArgs& args, int d, hipStream_t st) {
   }
   auto launch = [&](auto circle) {
     constexpr bool C = decltype(circle)::value;
-    if (d == 128) window_fwd_bf16<128, 2, 4, C><<<grid, 64 * NW, 0, st>>>(a);
-    else window_fwd_bf16<64, 3, 4, C><<<grid, 64 * NW, 0, st>>>(a);
+    if (d == 128) window_fwd_bf16<128, 2, 2, 4, C><<<grid, 128, 0, st>>>(a);
+    else window_fwd_bf16<64, 2, 3, 4, C><<<grid, 128, 0, st>>>(a);
   };
   a.by_period = div_by(a.period);
   window_slots(&a, kWindowRows);
-  if (a.period > 0) launch(std::true_type{});
+  // Four waves a workgroup where two would leave half of the SIMDs idle (two workgroups a CU or fewer), and the lists are long enough for the second
+  // merge.  Two / four waves: 4 heads of 500 tokens 16.6 / 13.4 us, d = 64, left 127 12.1 / 9.7; 16 heads of 2000, left 300 (512 workgroups) 21.6 / 19.3, d = 64 16.7 / 13.1; 24
+  // heads (768) 23.8 / 28.8; lists of 60 keys 8.9 / 10.4, of 130 and 190 that all see 11.6 / 12.2 and 11.4 / 12.0; d = 64, 100 tokens 8.5 / 7.6, 60 6.6 / 7.4.
+  if ((long long)grid.x * grid.y <= 512 && window_most_keys(a.w, kWindowRows) / a.splits > (d == 128 ? 192 : 64)) {
+    if (d == 128) window_fwd_bf16<128, 4, 2, 4, false><<<grid, 256, 0, st>>>(a);
+    else window_fwd_bf16<64, 4, 3, 4, false><<<grid, 256, 0, st>>>(a);
+  } else if (a.period > 0) launch(std::true_type{});
   else launch(std::false_type{});
   return hipGetLastError();
 }

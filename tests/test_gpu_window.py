@@ -186,6 +186,21 @@ def test_long_windows_of_many_rows(usv, d, left, right, sinks, chunk):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H, L", [(3, 1100), (24, 1500)])
+@pytest.mark.parametrize("left, right, sinks, chunk", [(-1, 0, 0, 1), (-1, -1, 0, 1), (300, 0, 100, 1), (1, 1, 1, 130), (40, 3, 64, 1)])
+def test_workgroups_of_four_waves_and_of_two(usv, d, H, L, left, right, sinks, chunk):
+    """54 and 576 workgroups: fewer and more than there are places; lists of two to twenty-four tiles, not shared out."""
+    q, k, v = (normal((1, H, L, d), 230 + i, torch.bfloat16).to(DEV) for i in range(3))
+    none = torch.empty(0, dtype=torch.uint8, device=DEV)
+    out, lse = usv.window_attn(q, k, v, left, right, sinks, chunk, workspace=none, return_lse=True)
+    M = torch.from_numpy(wo.masks(1, L, L, left, right, sinks, chunk)[0]).to(DEV)
+    for h in range(0, H, 2):
+        ref, ls, mag = torch_rows(q[0, h], k[0, h], v[0, h], M, d ** -0.5)
+        close(out[0, h], f64(ref), f64(mag), "bf16", f"head {h}")
+        close_lse(lse[0, h], f64(ls))
+
+
+@pytest.mark.parametrize("d", [64, 128])
 def test_long_windows_of_few_rows(usv, d):
     """In one piece and shared out, from one row to a block and a bit, the first key of the list at any place of a tile."""
     L, left = 5000, 4300
